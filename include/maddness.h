@@ -78,6 +78,13 @@ enum {
     MADDNESS_FIT_SOFTMAX_SQERR = 4   /* row softmax, squared error (Eq. 3)        */
 };
 
+/* Element types of the output layer's matrices. */
+enum {
+    MADDNESS_F32 = 0,
+    MADDNESS_BF16 = 1,
+    MADDNESS_F16 = 2
+};
+
 #define MADDNESS_K 16          /* prototypes per codebook (4-bit indices)   */
 #define MADDNESS_LEVELS 4      /* tree depth: comparisons per codebook      */
 #define MADDNESS_NODES 15      /* thresholds per codebook                   */
@@ -390,6 +397,113 @@ int maddness_encoder_scatter(const uint8_t* idx, int64_t N, int32_t C,
                              const float* Y, int32_t M, double* out,
                              void* workspace, int64_t workspace_bytes,
                              void* stream);
+
+/*
+ * 4-bit block floating point weights (the 8-bit format of the tables, §1, at
+ * half the bits), for layers that keep their product: the matrix W [D][M]
+ * stands for B [D][M], 32 consecutive rows of a column sharing one power of
+ * two.  For the group's largest magnitude a (finite), e is the smallest
+ * integer in [-120, 125] with a <= 6 * 2^e, and each weight is the value of
+ * {0, 0.5, 1, 1.5, 2, 3, 4, 6} nearest to |B| * 2^-e (ties to the even code;
+ * 6 past the range) with B's sign, times 2^e.  A group with a value that is
+ * not finite becomes 32 NaN.
+ *
+ * Packed, with Mb = ceil(M / 16) and Kb = ceil(D / 128):
+ *   codes [Mb][Kb][64][16] uint8: bytes 4 j .. 4 j + 3 of entry (mb, kb, l)
+ *         hold the 8 codes, low bits first, of column 16 mb + l % 16, rows
+ *         128 kb + 32 j + 8 (l / 16) + 0..7.  Code: magnitude 0..7, sign in
+ *         bit 3.
+ *   exps  [Mb][Kb][16][4] uint8: e + 127 of rows 128 kb + 32 j + 0..31 of
+ *         column 16 mb + i at (mb, kb, i, j); 255: NaN.
+ * Rows and columns past the matrix hold code 0 and e = 0.
+ * The two functions give the arrays' sizes (-1 for sizes that are not
+ * positive).
+ */
+int64_t maddness_w4_code_bytes(int32_t D, int32_t M);
+int64_t maddness_w4_exponent_bytes(int32_t D, int32_t M);
+
+/*
+ * Quantizes B (dtype MADDNESS_F32, _BF16 or _F16; element (d, m) at
+ * d * stride_d + m * stride_m, strides in elements, not negative) into codes
+ * (16-byte aligned) and exps (4-byte aligned).  EINVAL: NULL, sizes that are
+ * not positive, another dtype, misaligned arrays.
+ */
+int maddness_quantize_w4(const void* B, int32_t dtype, int32_t D, int32_t M,
+                         int64_t stride_d, int64_t stride_m, uint8_t* codes_out,
+                         uint8_t* exps_out, void* stream);
+
+/* The weights that the codes stand for, B_out [D][M] dense, as fp32 or bf16
+   (both exact). */
+int maddness_dequantize_w4(const uint8_t* codes, const uint8_t* exps, int32_t D,
+                           int32_t M, void* B_out, int32_t dtype, void* stream);
+
+/*
+ * Layer with 4-bit weights: y = sigma(A W + col_bias), act as for
+ * maddness_matmul_act (a bias is not used with MADDNESS_ACT_NONE).
+ *   A      [N][lda], dtype fp32, bf16 or fp16; any alignment of its rows.
+ *   y_out  [N][M] dense, y_dtype fp32 or A's; a row softmax needs fp32.
+ * Products are exact (fp32 activations as three bf16 parts, fp16 as two) and
+ * summed in 32 bits, in an order that the shape fixes; y is rounded once.
+ * EINVAL: act or a dtype out of range, lda < D, a NULL array (when N > 0),
+ * codes not 16-byte or exps not 4-byte aligned.  N == 0 enqueues nothing.
+ */
+int maddness_matmul_w4(const void* A, int32_t dtype, int64_t N, int32_t D,
+                       int64_t lda, const uint8_t* codes, const uint8_t* exps,
+                       int32_t M, const float* col_bias, int32_t act, void* y_out,
+                       int32_t y_dtype, void* stream);
+
+/*
+ * Softmax cross entropy of an output layer, without keeping its logits: with
+ * z = A B + col_bias,
+ *   lse[n]  = log sum_m exp(z[n][m])
+ *   loss[n] = lse[n] - z[n][target[n]].
+ * (maddness_fit_lut_gd fits tables under a softmax of few columns; this is the
+ * loss of the layer's own weights, for any number of outputs.)
+ *   A       [N][lda], dtype MADDNESS_F32 or MADDNESS_BF16.
+ *   B       the same dtype, dense: [D][M], or [M][D] with outputs_first = 1.
+ *   col_bias [M] fp32 or NULL; -inf switches an output off.
+ *   target  [N] int64.  A row whose target is outside [0, M) has no loss: 0,
+ *           and no gradient.
+ *   loss_out, lse_out [N] fp32.  A row without any finite logit: lse -inf,
+ *           loss +inf, no gradient.  A target that is switched off: loss +inf.
+ * Logits are summed and exponentiated in 32 bits; fp32 matrices are multiplied
+ * as three bf16 parts each, the terms below 2^-24 of a product left out.
+ * Values of A and B that are not finite make the rows they meet NaN.
+ * workspace: at least maddness_linear_xent_workspace_bytes(N, D, M, dtype)
+ * device bytes, 256-byte aligned, contents undefined on return.
+ * EINVAL: a NULL array (when N > 0), bad sizes, dtype, alignment or workspace;
+ * EUNSUPPORTED: N >= 2^31.  N == 0 enqueues nothing.
+ */
+int64_t maddness_linear_xent_workspace_bytes(int64_t N, int32_t D, int32_t M,
+                                             int32_t dtype);   /* -1 if out of range */
+int maddness_linear_xent(const void* A, int32_t dtype, int64_t N, int32_t D,
+                         int64_t lda, const void* B, int32_t M,
+                         int32_t outputs_first, const float* col_bias,
+                         const int64_t* target, float* loss_out, float* lse_out,
+                         void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The gradient of sum_n grad_loss[n] * loss[n]: with
+ *   G[n][m] = grad_loss[n] (exp(z[n][m] - lse[n]) - [m == target[n]])
+ * (0 for rows without a gradient),
+ *   dA = G B^T [N][D], dB = A^T G (laid out like B), dbias[m] = sum_n G[n][m].
+ * lse as maddness_linear_xent gives it; z is formed again.  dA and dB have A's
+ * dtype, dense; with bf16, G is rounded to bf16 for the two products (as A
+ * and B are), which are summed in 32 bits and rounded once; dbias [M] is fp32
+ * from the unrounded G.  Sums have an order that the shape fixes: the same
+ * call gives the same bits.  The outputs are taken in pieces, so workspace
+ * (maddness_linear_xent_grad_workspace_bytes) stays far below the logits.
+ * N == 0 writes zeros to dB and dbias.  Errors as above.
+ */
+int64_t maddness_linear_xent_grad_workspace_bytes(int64_t N, int32_t D, int32_t M,
+                                                  int32_t dtype);   /* -1 if out of range */
+int maddness_linear_xent_grad(const void* A, int32_t dtype, int64_t N, int32_t D,
+                              int64_t lda, const void* B, int32_t M,
+                              int32_t outputs_first, const float* col_bias,
+                              const int64_t* target, const float* lse,
+                              const float* grad_loss, void* dA_out, void* dB_out,
+                              float* dbias_out, void* workspace,
+                              int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

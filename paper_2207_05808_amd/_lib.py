@@ -73,7 +73,20 @@ def lib() -> ctypes.CDLL:
         L.maddness_fit_lut_gd_workspace_bytes.restype = i64
         L.maddness_fit_lut_gd.argtypes = [vp, i64, i32, vp, i32, vp, i32, vp, ctypes.c_double, ctypes.c_double, i32,
                                           vp, vp, i64, vp]
-        for f in ("maddness_version", "maddness_encode", "maddness_lut_accumulate",
+        L.maddness_w4_code_bytes.argtypes = [i32, i32]
+        L.maddness_w4_code_bytes.restype = i64
+        L.maddness_w4_exponent_bytes.argtypes = [i32, i32]
+        L.maddness_w4_exponent_bytes.restype = i64
+        L.maddness_quantize_w4.argtypes = [vp, i32, i32, i32, i64, i64, vp, vp, vp]
+        L.maddness_dequantize_w4.argtypes = [vp, vp, i32, i32, vp, i32, vp]
+        L.maddness_matmul_w4.argtypes = [vp, i32, i64, i32, i64, vp, vp, i32, vp, i32, vp, i32, vp]
+        for f in ("maddness_linear_xent_workspace_bytes", "maddness_linear_xent_grad_workspace_bytes"):
+            getattr(L, f).argtypes = [i64, i32, i32, i32]
+            getattr(L, f).restype = i64
+        L.maddness_linear_xent.argtypes = [vp, i32, i64, i32, i64, vp, i32, i32, vp, vp, vp, vp, vp, i64, vp]
+        L.maddness_linear_xent_grad.argtypes = [vp, i32, i64, i32, i64, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        for f in ("maddness_quantize_w4", "maddness_dequantize_w4", "maddness_matmul_w4", "maddness_linear_xent",
+                  "maddness_linear_xent_grad", "maddness_version", "maddness_encode", "maddness_lut_accumulate",
                   "maddness_lut_accumulate_f32", "maddness_matmul", "maddness_matmul_f32",
                   "maddness_matmul_act", "maddness_matmul_act_f32", "maddness_build_lut",
                   "maddness_build_lut_f32", "maddness_lut_accumulate_avg", "maddness_build_lut_shared",

@@ -11,8 +11,9 @@ for tests and debugging.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -681,3 +682,244 @@ def fit_lut_gd_workspace_bytes(N: int, C: int, M: int) -> int:
     if n < 0:
         _lib.check("maddness_fit_lut_gd_workspace_bytes", _lib.EUNSUPPORTED)
     return n
+
+
+# ------------------------------------------------- the output layer's operators
+
+# element types (MADDNESS_F32, _BF16, _F16)
+DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _typed(t, name: str, dtypes, ndim: int) -> int:
+    """Checks a device tensor of one of these types; returns the ABI's code."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be one of {', '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    _need(t, name, t.dtype, ndim)
+    return DTYPE[t.dtype]
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} must be on {device}, got {t.device}")
+
+
+@contextlib.contextmanager
+def _device(device):
+    """The device of the call's tensors as the current one."""
+    if device.index == torch.cuda.current_device():
+        yield
+    else:
+        with torch.cuda.device(device):
+            yield
+
+
+def _row_stride(A) -> int:
+    """Elements between A's rows, whose columns must be dense."""
+    N, D = A.shape
+    if D > 1 and N > 0 and A.stride(1) != 1:
+        raise ValueError("A must have unit column stride")
+    if N > 1 and A.stride(0) < D:
+        raise ValueError("A's rows must not overlap")
+    return A.stride(0) if N > 1 else D
+
+
+def _scratch(workspace, need: int, device, stream):
+    """_workspace of a caller's tensor checked for type and device."""
+    if workspace is not None:
+        _need(workspace, "workspace", torch.uint8, 1)
+        _dense(workspace, "workspace")
+        _same_device(device, workspace=workspace)
+    return _workspace(workspace, need, device, stream)
+
+
+def _output(t, name: str, shape, dtype, device):
+    """The caller's output tensor checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _need(t, name, dtype, len(shape))
+    _dense(t, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    _same_device(device, **{name: t})
+    return t
+
+
+class W4Weights(NamedTuple):
+    """4-bit block floating point weights of a layer [D, M] in the packed
+    layout of include/maddness.h: codes uint8 [ceil(M / 16), ceil(D / 128), 64,
+    16] and exps uint8 [ceil(M / 16), ceil(D / 128), 16, 4]."""
+    codes: torch.Tensor
+    exps: torch.Tensor
+    D: int
+    M: int
+
+
+def _w4(w):
+    if not isinstance(w, W4Weights):
+        raise TypeError("weights must be W4Weights (quantize_w4 makes them)")
+    _need(w.codes, "codes", torch.uint8, 4)
+    _need(w.exps, "exps", torch.uint8, 4)
+    _dense(w.codes, "codes")
+    _dense(w.exps, "exps")
+    D, M = int(w.D), int(w.M)
+    if D <= 0 or M <= 0:
+        raise ValueError("D and M must be positive")
+    blocks = ((M + 15) // 16, (D + 127) // 128)
+    if tuple(w.codes.shape) != blocks + (64, 16) or tuple(w.exps.shape) != blocks + (16, 4):
+        raise ValueError(f"weights of [{D}, {M}] have codes {list(blocks + (64, 16))} and exps {list(blocks + (16, 4))}, "
+                         f"got {list(w.codes.shape)} and {list(w.exps.shape)}")
+    _same_device(w.codes.device, exps=w.exps)
+    return D, M
+
+
+def quantize_w4(B, stream=None) -> W4Weights:
+    """4-bit block floating point weights of B [D, M] (fp32, bf16 or fp16, any
+    strides); see maddness_quantize_w4."""
+    code = _typed(B, "B", (torch.float32, torch.bfloat16, torch.float16), 2)
+    D, M = B.shape
+    if D == 0 or M == 0:
+        raise ValueError("B must not be empty")
+    blocks = ((M + 15) // 16, (D + 127) // 128)
+    with _device(B.device):
+        codes = torch.empty(blocks + (64, 16), dtype=torch.uint8, device=B.device)
+        exps = torch.empty(blocks + (16, 4), dtype=torch.uint8, device=B.device)
+        st = _lib.lib().maddness_quantize_w4(_ptr(B), code, D, M, B.stride(0), B.stride(1), _ptr(codes), _ptr(exps),
+                                             _stream(stream))
+    _lib.check("maddness_quantize_w4", st)
+    return W4Weights(codes, exps, D, M)
+
+
+def dequantize_w4(w: W4Weights, dtype=torch.bfloat16, out=None, stream=None):
+    """The weights [D, M] that the codes stand for, as bf16 or fp32 (both exact)."""
+    D, M = _w4(w)
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"dtype must be torch.float32 or torch.bfloat16, got {dtype}")
+    with _device(w.codes.device):
+        out = _output(out, "out", (D, M), dtype, w.codes.device)
+        st = _lib.lib().maddness_dequantize_w4(_ptr(w.codes), _ptr(w.exps), D, M, _ptr(out), DTYPE[dtype], _stream(stream))
+    _lib.check("maddness_dequantize_w4", st)
+    return out
+
+
+def matmul_w4(A, w: W4Weights, col_bias=None, act=None, out_dtype=None, y_out=None, stream=None):
+    """Layer with 4-bit weights, sigma(A W + col_bias); returns y [N, M].
+
+    A [N, D] fp32, bf16 or fp16 with dense columns.  act "none" (no bias),
+    "bias", "relu" or "softmax"; None: "bias" where one is given.  y has A's
+    dtype, or out_dtype torch.float32, which a softmax always gives."""
+    code = _typed(A, "A", (torch.float32, torch.bfloat16, torch.float16), 2)
+    D, M = _w4(w)
+    N = A.shape[0]
+    if A.shape[1] != D:
+        raise ValueError(f"A must have the weights' {D} columns, got {A.shape[1]}")
+    lda = _row_stride(A)
+    col_bias = _col_bias(col_bias, M)
+    _same_device(A.device, weights=w.codes, col_bias=col_bias)
+    a = _act(act if act is not None else "none" if col_bias is None else "bias")
+    if out_dtype is None:
+        out_dtype = y_out.dtype if y_out is not None else torch.float32 if a == ACT["softmax"] else A.dtype
+    if out_dtype not in (A.dtype, torch.float32):
+        raise TypeError(f"out_dtype must be {A.dtype} or torch.float32, got {out_dtype}")
+    if a == ACT["softmax"] and out_dtype != torch.float32:
+        raise TypeError("a softmax gives torch.float32")
+    with _device(A.device):
+        y_out = _output(y_out, "y_out", (N, M), out_dtype, A.device)
+        st = _lib.lib().maddness_matmul_w4(_ptr(A), code, N, D, lda, _ptr(w.codes), _ptr(w.exps), M, _ptr(col_bias), a,
+                                           _ptr(y_out), DTYPE[out_dtype], _stream(stream))
+    _lib.check("maddness_matmul_w4", st)
+    return y_out
+
+
+def _xent_inputs(A, B, target, col_bias):
+    code = _typed(A, "A", (torch.float32, torch.bfloat16), 2)
+    _need(B, "B", A.dtype, 2)
+    _need(target, "target", torch.int64, 1)
+    _dense(target, "target")
+    N, D = A.shape
+    M = B.shape[1]
+    if D == 0 or M == 0:
+        raise ValueError("A and B must have columns")
+    if B.shape[0] != D or target.shape[0] != N:
+        raise ValueError(f"A [N, D], B [D, M] and target [N] do not fit: {list(A.shape)}, {list(B.shape)}, {list(target.shape)}")
+    if not B.is_contiguous() and not B.t().is_contiguous():
+        raise ValueError("B must be contiguous, or the transpose of a contiguous tensor")
+    first = 0 if B.is_contiguous() else 1
+    col_bias = _col_bias(col_bias, M)
+    _same_device(A.device, B=B, target=target, col_bias=col_bias)
+    return code, N, D, M, _row_stride(A), first, col_bias
+
+
+def linear_xent(A, B, target, col_bias=None, loss_out=None, lse_out=None, workspace=None, stream=None):
+    """Softmax cross entropy of the output layer A B + col_bias without keeping
+    the logits; returns (loss [N], lse [N]) in fp32.
+
+    A [N, D] and B [D, M] fp32 or bf16 (B contiguous, or the transpose of a
+    contiguous [M, D]); target [N] int64, outside [0, M) for rows without a
+    loss.  ``workspace``: an optional uint8 device tensor of at least
+    linear_xent_workspace_bytes(N, D, M, A.dtype) bytes (+ up to 255 for
+    alignment)."""
+    code, N, D, M, lda, first, col_bias = _xent_inputs(A, B, target, col_bias)
+    with _device(A.device):
+        loss_out = _output(loss_out, "loss_out", (N,), torch.float32, A.device)
+        lse_out = _output(lse_out, "lse_out", (N,), torch.float32, A.device)
+        need = linear_xent_workspace_bytes(N, D, M, A.dtype)
+        workspace, wp = _scratch(workspace, need, A.device, stream)
+        st = _lib.lib().maddness_linear_xent(_ptr(A), code, N, D, lda, _ptr(B), M, first, _ptr(col_bias), _ptr(target),
+                                             _ptr(loss_out), _ptr(lse_out), wp, need, _stream(stream))
+    _lib.check("maddness_linear_xent", st)
+    return loss_out, lse_out
+
+
+def linear_xent_grad(A, B, target, lse, grad_loss, col_bias=None, dA_out=None, dB_out=None, dbias_out=None, workspace=None,
+                     stream=None):
+    """The gradient of (grad_loss * loss).sum(): returns (dA [N, D], dB [D, M],
+    dbias [M]); dA and dB in A's dtype, dB laid out like B, dbias fp32.
+
+    lse [N] as linear_xent gave it for the same A, B, target and col_bias;
+    grad_loss [N] fp32.  ``workspace``: an optional uint8 device tensor of at
+    least linear_xent_grad_workspace_bytes(N, D, M, A.dtype) bytes (+ up to 255
+    for alignment)."""
+    code, N, D, M, lda, first, col_bias = _xent_inputs(A, B, target, col_bias)
+    for t, name in ((lse, "lse"), (grad_loss, "grad_loss")):
+        _need(t, name, torch.float32, 1)
+        _dense(t, name)
+        if t.shape[0] != N:
+            raise ValueError(f"{name} must be [N]")
+    _same_device(A.device, lse=lse, grad_loss=grad_loss)
+    with _device(A.device):
+        dA_out = _output(dA_out, "dA_out", (N, D), A.dtype, A.device)
+        if dB_out is not None and first:
+            _need(dB_out, "dB_out", A.dtype, 2)
+            _output(dB_out.t(), "dB_out's transpose", (M, D), A.dtype, A.device)
+        elif first:
+            dB_out = torch.empty((M, D), dtype=A.dtype, device=A.device).t()
+        else:
+            dB_out = _output(dB_out, "dB_out", (D, M), A.dtype, A.device)
+        dbias_out = _output(dbias_out, "dbias_out", (M,), torch.float32, A.device)
+        need = linear_xent_grad_workspace_bytes(N, D, M, A.dtype)
+        workspace, wp = _scratch(workspace, need, A.device, stream)
+        st = _lib.lib().maddness_linear_xent_grad(_ptr(A), code, N, D, lda, _ptr(B), M, first, _ptr(col_bias), _ptr(target),
+                                                  _ptr(lse), _ptr(grad_loss), _ptr(dA_out), _ptr(dB_out), _ptr(dbias_out),
+                                                  wp, need, _stream(stream))
+    _lib.check("maddness_linear_xent_grad", st)
+    return dA_out, dB_out, dbias_out
+
+
+def _xent_bytes(fn, N, D, M, dtype) -> int:
+    n = int(getattr(_lib.lib(), fn)(N, D, M, DTYPE.get(dtype, -1)))
+    if n < 0:
+        _lib.check(fn, _lib.EUNSUPPORTED)
+    return n
+
+
+def linear_xent_workspace_bytes(N: int, D: int, M: int, dtype=torch.float32) -> int:
+    """Device bytes linear_xent needs as workspace."""
+    return _xent_bytes("maddness_linear_xent_workspace_bytes", N, D, M, dtype)
+
+
+def linear_xent_grad_workspace_bytes(N: int, D: int, M: int, dtype=torch.float32) -> int:
+    """Device bytes linear_xent_grad needs as workspace."""
+    return _xent_bytes("maddness_linear_xent_grad_workspace_bytes", N, D, M, dtype)

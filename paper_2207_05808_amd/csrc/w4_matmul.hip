@@ -1,0 +1,337 @@
+// Products with 4-bit block floating point weights, their quantizer, and the
+// way back (maddness_quantize_w4, maddness_dequantize_w4, maddness_matmul_w4;
+// the format is described in include/maddness.h).
+//
+// A weight is an E2M1 code times 2^e, e shared by 32 rows of a column.  Two
+// bits of mantissa times a power of two are exact in bf16, and one instruction
+// unpacks two codes and scales them, so a weight costs half an instruction and
+// the scale none after the product.
+#include "maddness.h"
+#include "internal.hpp"
+#include "mma.hpp"
+
+namespace mdn {
+namespace {
+
+constexpr int kWK = 128, kWM = 16;   // rows and columns of a packed block: 64 lanes x 16 bytes
+
+// the 8 codes of one word as bf16, times the power of two
+__device__ __forceinline__ bf16x8 unpack8(uint32_t w, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  return (bf16x8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// biased exponent byte j as the power of two it stands for (255: NaN weights)
+__device__ __forceinline__ float scale_of(uint32_t exps, int j) {
+  return __uint_as_float(((exps >> (8 * j)) & 0xffu) << 23);
+}
+
+// 8 consecutive values of a row as bf16 parts; values at or past `left` are 0
+template <class T>
+__device__ __forceinline__ void load_parts(const T* p, int left, bf16x8 (&out)[Parts<T>::n]) {
+  constexpr int P = Parts<T>::n;
+  if constexpr (P == 1) {
+    u32x4 v = {0, 0, 0, 0};
+    if (left >= 8) {
+      v = load16(p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < left) v[i >> 1] |= (uint32_t)p[i].bits << (16 * (i & 1));
+    }
+    out[0] = __builtin_bit_cast(bf16x8, v);
+  } else {
+    float f[8];
+    if (left >= 8) {
+      if constexpr (sizeof(T) == 4) {
+        const u32x4 a = load16(p), b = load16(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[i] = __uint_as_float(a[i]); f[4 + i] = __uint_as_float(b[i]); }
+      } else {
+        const u32x4 a = load16(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = to_float(T{(uint16_t)(a[i >> 1] >> (16 * (i & 1)))});
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = i < left ? to_float(p[i]) : 0.0f;
+    }
+    u32x4 w[P];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t q[P];
+      split2<P>(f[2 * i], f[2 * i + 1], q);
+#pragma unroll
+      for (int s = 0; s < P; ++s) w[s][i] = q[s];
+    }
+#pragma unroll
+    for (int s = 0; s < P; ++s) out[s] = __builtin_bit_cast(bf16x8, w[s]);
+  }
+}
+
+struct WArgs {
+  const void* A; int64_t N, lda; int D, M;
+  const uint8_t* codes; const uint8_t* exps;
+  const float* bias; int act;   // 0 none, 1 bias, 2 bias + ReLU (a row softmax is a second pass)
+  void* y;
+  int nk, nm;                   // blocks of 128 rows / 16 columns of the weights
+};
+
+__device__ __forceinline__ float w4_sigma(const WArgs& a, float v, int m) {
+  if (a.bias) v += a.bias[m];
+  return a.act == 2 ? (v > 0.0f ? v : 0.0f) : v;
+}
+
+// One workgroup: 16 columns x 16 RT rows, the wavefronts taking the weight's
+// 128-row blocks in turn and their sums added through LDS.
+template <class T, class Y, int RT>
+__global__ void __launch_bounds__(512) w4_rows_kernel(WArgs a) {
+  constexpr int P = Parts<T>::n;
+  extern __shared__ float red[];   // [wavefronts][RT][16 rows][16 columns]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int col = lane & 15, quarter = lane >> 4;
+  const int mb = blockIdx.x;
+  const u32x4* codes = reinterpret_cast<const u32x4*>(a.codes) + (int64_t)mb * a.nk * 64 + lane;
+  const uint32_t* exps = reinterpret_cast<const uint32_t*>(a.exps) + (int64_t)mb * a.nk * 16 + col;
+  const int64_t chunks = (a.N + 16 * RT - 1) / (16 * RT);
+  for (int64_t c = blockIdx.y; c < chunks; c += gridDim.y) {
+    const int64_t n0 = c * (16 * RT);
+    f32x4 acc[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[r] = (f32x4){0, 0, 0, 0};
+    for (int kb = wave; kb < a.nk; kb += waves) {
+      const u32x4 w = codes[(int64_t)kb * 64];
+      const uint32_t e = exps[kb * 16];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x8 b = unpack8(w[j], scale_of(e, j));
+        const int k = kb * kWK + 32 * j + 8 * quarter;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          const int64_t n = n0 + 16 * r + col;
+          bf16x8 x[P];
+          load_parts(static_cast<const T*>(a.A) + n * a.lda + k, n < a.N ? a.D - k : 0, x);
+#pragma unroll
+          for (int p = P - 1; p >= 0; --p) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[p], b, acc[r], 0, 0, 0);
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) red[((wave * RT + r) * 16 + 4 * quarter + i) * 16 + col] = acc[r][i];
+    __syncthreads();
+    for (int t = threadIdx.x; t < RT * 256; t += blockDim.x) {
+      float v = red[t];
+      for (int w = 1; w < waves; ++w) v += red[w * RT * 256 + t];
+      const int64_t n = n0 + (t >> 4);
+      const int m = mb * kWM + (t & 15);
+      if (n < a.N && m < a.M) static_cast<Y*>(a.y)[n * a.M + m] = from_float<Y>(w4_sigma(a, v, m));
+    }
+    __syncthreads();
+  }
+}
+
+// Row softmax in place, one workgroup per row: three passes over a row that
+// stays in the L2.
+__global__ void __launch_bounds__(1024) w4_softmax_kernel(float* y, int64_t N, int M) {
+  __shared__ float part[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  for (int64_t n = blockIdx.x; n < N; n += gridDim.x) {
+    float* row = y + n * M;
+    float top = -__builtin_inff();
+    for (int m = threadIdx.x; m < M; m += blockDim.x) top = __builtin_fmaxf(top, row[m]);
+    for (int o = 1; o < 64; o <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
+    if (lane == 0) part[wave] = top;
+    __syncthreads();
+    for (int w = 0; w < waves; ++w) top = __builtin_fmaxf(top, part[w]);
+    __syncthreads();
+    float sum = 0.0f;
+    for (int m = threadIdx.x; m < M; m += blockDim.x) sum += expf(row[m] - top);
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    sum = 0.0f;
+    for (int w = 0; w < waves; ++w) sum += part[w];
+    __syncthreads();
+    for (int m = threadIdx.x; m < M; m += blockDim.x) row[m] = expf(row[m] - top) / sum;
+  }
+}
+
+struct QArgs {
+  const void* B; int64_t sd, sm;   // element (d, m) at d * sd + m * sm
+  int D, M, nk, nm;
+  uint8_t* codes; uint8_t* exps;
+};
+
+// One wavefront per packed block.  Lane (quarter, column) holds the 32 weights
+// that it will write: 8 rows of each of the block's four groups.
+template <class T>
+__global__ void __launch_bounds__(256) w4_quantize_kernel(QArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int col = lane & 15, quarter = lane >> 4;
+  const int64_t blocks = (int64_t)a.nk * a.nm;
+  for (int64_t b = (int64_t)blockIdx.x * 4 + wave; b < blocks; b += (int64_t)gridDim.x * 4) {
+    const int mb = (int)(b % a.nm), kb = (int)(b / a.nm);   // neighbours share the lines of B's rows
+    const int m = mb * kWM + col;
+    const T* src = static_cast<const T*>(a.B) + m * a.sm;
+    u32x4 word = {0, 0, 0, 0};
+    uint32_t exps = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float v[8], top = 0.0f;
+      bool odd = false;   // not finite
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int d = kb * kWK + 32 * j + 8 * quarter + i;
+        v[i] = d < a.D && m < a.M ? to_float(src[d * a.sd]) : 0.0f;
+        top = __builtin_fmaxf(top, __builtin_fabsf(v[i]));
+        odd = odd || !(__builtin_fabsf(v[i]) < __builtin_inff());
+      }
+      top = __builtin_fmaxf(top, __shfl_xor(top, 16));
+      top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+      int bad = odd;
+      bad |= __shfl_xor(bad, 16);
+      bad |= __shfl_xor(bad, 32);
+      // the smallest e with top <= 6 2^e: top = f 2^x, 1/2 <= f < 1, and 6 2^e = 3/4 2^(e + 3)
+      int x = 0;
+      const float f = frexpf(top, &x);
+      int e = f <= 0.75f ? x - 3 : x - 2;
+      e = top == 0.0f ? (kb * kWK + 32 * j < a.D && m < a.M ? -120 : 0) : e < -120 ? -120 : e > 125 ? 125 : e;
+      exps |= (uint32_t)(bad ? 255 : e + 127) << (8 * j);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float t = ldexpf(__builtin_fabsf(v[i]), -e);   // (exact, or far below the first edge)
+        uint32_t q = (t > 0.25f) + (t >= 0.75f) + (t > 1.25f) + (t >= 1.75f) + (t > 2.5f) + (t >= 3.5f) + (t > 5.0f);
+        q = bad ? 0 : q && v[i] < 0.0f ? q + 8 : q;
+        word[j] |= q << (4 * i);
+      }
+    }
+    const int64_t at = (int64_t)mb * a.nk + kb;
+    reinterpret_cast<u32x4*>(a.codes)[at * 64 + lane] = word;
+    if (quarter == 0) reinterpret_cast<uint32_t*>(a.exps)[at * 16 + col] = exps;
+  }
+}
+
+struct DArgs {
+  const uint8_t* codes; const uint8_t* exps; int D, M, nk, nm;
+  void* B;   // [D][M]
+};
+
+template <class T>
+__global__ void __launch_bounds__(256) w4_dequantize_kernel(DArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int col = lane & 15, quarter = lane >> 4;
+  const int64_t blocks = (int64_t)a.nk * a.nm;
+  for (int64_t b = (int64_t)blockIdx.x * 4 + wave; b < blocks; b += (int64_t)gridDim.x * 4) {
+    const int mb = (int)(b % a.nm), kb = (int)(b / a.nm);
+    const int m = mb * kWM + col;
+    const int64_t at = (int64_t)mb * a.nk + kb;
+    const u32x4 w = reinterpret_cast<const u32x4*>(a.codes)[at * 64 + lane];
+    const uint32_t e = reinterpret_cast<const uint32_t*>(a.exps)[at * 16 + col];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bf16x8 v = unpack8(w[j], scale_of(e, j));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int d = kb * kWK + 32 * j + 8 * quarter + i;
+        if (d < a.D && m < a.M) static_cast<T*>(a.B)[(int64_t)d * a.M + m] = from_float<T>((float)v[i]);
+      }
+    }
+  }
+}
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+int status_from(hipError_t e) { return e == hipSuccess ? MADDNESS_OK : MADDNESS_EHIP; }
+int blocks_for(int64_t waves, int per) {
+  const int64_t b = (waves + per - 1) / per, most = 1 << 20;
+  return (int)(b < most ? b : most);
+}
+
+template <class T, class Y, int RT>
+hipError_t launch_rows(const WArgs& a, hipStream_t stream) {
+  const int waves = a.nk < 8 ? a.nk : 8;
+  const int64_t chunks = (a.N + 16 * RT - 1) / (16 * RT);
+  hipLaunchKernelGGL((w4_rows_kernel<T, Y, RT>), dim3((unsigned)a.nm, (unsigned)(chunks < 65535 ? chunks : 65535)), dim3(64 * waves),
+                     waves * RT * 1024, stream, a);
+  return hipGetLastError();
+}
+
+template <class T, class Y>
+hipError_t launch_w4(const WArgs& a, hipStream_t stream) {
+  if (a.N <= 16) return launch_rows<T, Y, 1>(a, stream);
+  if (a.N <= 32) return launch_rows<T, Y, 2>(a, stream);
+  return launch_rows<T, Y, 4>(a, stream);
+}
+
+}  // namespace
+}  // namespace mdn
+
+using namespace mdn;
+
+extern "C" {
+
+int64_t maddness_w4_code_bytes(int32_t D, int32_t M) {
+  if (D <= 0 || M <= 0) return -1;
+  return (((int64_t)D + kWK - 1) / kWK) * (((int64_t)M + kWM - 1) / kWM) * 1024;
+}
+
+int64_t maddness_w4_exponent_bytes(int32_t D, int32_t M) {
+  const int64_t n = maddness_w4_code_bytes(D, M);
+  return n < 0 ? -1 : n / 16;
+}
+
+int maddness_quantize_w4(const void* B, int32_t dtype, int32_t D, int32_t M, int64_t stride_d, int64_t stride_m,
+                         uint8_t* codes_out, uint8_t* exps_out, void* stream) {
+  if (D <= 0 || M <= 0 || stride_d < 0 || stride_m < 0 || !B || !codes_out || !exps_out) return MADDNESS_EINVAL;
+  if (dtype < MADDNESS_F32 || dtype > MADDNESS_F16) return MADDNESS_EINVAL;
+  if (!aligned(B, dtype == MADDNESS_F32 ? 4 : 2) || !aligned(codes_out, 16) || !aligned(exps_out, 4)) return MADDNESS_EINVAL;
+  QArgs a{B, stride_d, stride_m, D, M, (int)(((int64_t)D + kWK - 1) / kWK), (int)(((int64_t)M + kWM - 1) / kWM), codes_out, exps_out};
+  const dim3 grid(blocks_for((int64_t)a.nk * a.nm, 4));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (dtype == MADDNESS_F32) hipLaunchKernelGGL((w4_quantize_kernel<float>), grid, dim3(256), 0, s, a);
+  else if (dtype == MADDNESS_BF16) hipLaunchKernelGGL((w4_quantize_kernel<Bf16>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((w4_quantize_kernel<F16>), grid, dim3(256), 0, s, a);
+  return status_from(hipGetLastError());
+}
+
+int maddness_dequantize_w4(const uint8_t* codes, const uint8_t* exps, int32_t D, int32_t M, void* B_out, int32_t dtype,
+                           void* stream) {
+  if (D <= 0 || M <= 0 || !codes || !exps || !B_out) return MADDNESS_EINVAL;
+  if (dtype != MADDNESS_F32 && dtype != MADDNESS_BF16) return MADDNESS_EINVAL;
+  if (!aligned(B_out, dtype == MADDNESS_F32 ? 4 : 2) || !aligned(codes, 16) || !aligned(exps, 4)) return MADDNESS_EINVAL;
+  DArgs a{codes, exps, D, M, (int)(((int64_t)D + kWK - 1) / kWK), (int)(((int64_t)M + kWM - 1) / kWM), B_out};
+  const dim3 grid(blocks_for((int64_t)a.nk * a.nm, 4));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (dtype == MADDNESS_F32) hipLaunchKernelGGL((w4_dequantize_kernel<float>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((w4_dequantize_kernel<Bf16>), grid, dim3(256), 0, s, a);
+  return status_from(hipGetLastError());
+}
+
+int maddness_matmul_w4(const void* A, int32_t dtype, int64_t N, int32_t D, int64_t lda, const uint8_t* codes,
+                       const uint8_t* exps, int32_t M, const float* col_bias, int32_t act, void* y_out,
+                       int32_t y_dtype, void* stream) {
+  if (N < 0 || D <= 0 || M <= 0 || lda < D || act < 0 || act > 3) return MADDNESS_EINVAL;
+  if (dtype < MADDNESS_F32 || dtype > MADDNESS_F16 || (y_dtype != dtype && y_dtype != MADDNESS_F32)) return MADDNESS_EINVAL;
+  if (act == MADDNESS_ACT_SOFTMAX && y_dtype != MADDNESS_F32) return MADDNESS_EINVAL;
+  if (N == 0) return MADDNESS_OK;
+  if (!A || !codes || !exps || !y_out) return MADDNESS_EINVAL;
+  if (!aligned(A, dtype == MADDNESS_F32 ? 4 : 2) || !aligned(y_out, y_dtype == MADDNESS_F32 ? 4 : 2) || !aligned(codes, 16) ||
+      !aligned(exps, 4) || (col_bias && !aligned(col_bias, 4)))
+    return MADDNESS_EINVAL;
+  WArgs a{A, N, lda, D, M, codes, exps, act == MADDNESS_ACT_NONE ? nullptr : col_bias, act == MADDNESS_ACT_RELU ? 2 : 0, y_out,
+          (int)(((int64_t)D + kWK - 1) / kWK), (int)(((int64_t)M + kWM - 1) / kWM)};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  if (dtype == MADDNESS_F32) e = launch_w4<float, float>(a, s);
+  else if (dtype == MADDNESS_BF16) e = y_dtype == MADDNESS_F32 ? launch_w4<Bf16, float>(a, s) : launch_w4<Bf16, Bf16>(a, s);
+  else e = y_dtype == MADDNESS_F32 ? launch_w4<F16, float>(a, s) : launch_w4<F16, F16>(a, s);
+  if (e != hipSuccess || act != MADDNESS_ACT_SOFTMAX) return status_from(e);
+  hipLaunchKernelGGL(w4_softmax_kernel, dim3((unsigned)(N < 65535 ? N : 65535)), dim3(1024), 0, s, static_cast<float*>(y_out), N, M);
+  return status_from(hipGetLastError());
+}
+
+}  // extern "C"
