@@ -15,6 +15,8 @@
 #include "internal.hpp"
 #include "mma.hpp"
 
+#include <type_traits>
+
 namespace mdn {
 namespace {
 
@@ -24,14 +26,16 @@ struct Operand {
   const void* p;
   int64_t ld;     // elements between rows (kAlongK) or between k steps (kAlongI)
   int64_t rows;   // extent of the operand's own index
+  int64_t pad;    // what of it memory holds (kAlongI: whole 16-byte units from `rows` on)
 };
 
 // A tile of BI x BJ results of one workgroup of WI x WJ wavefronts, k in steps
 // of BK through two LDS buffers.
-template <class T, Order OX, Order OY, int BI, int BJ, int WI, int WJ>
+template <class T, Order OX, Order OY, int BI_, int BJ_, int WI_, int WJ_, int BK_ = sizeof(T) == 2 ? 64 : 32>
 struct Tile {
+  static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_;
   static constexpr int P = Parts<T>::n;
-  static constexpr int BK = P == 1 ? 64 : 32;
+  static constexpr int BK = BK_;
   static constexpr int CH = 16 / sizeof(T);          // elements of a 16-byte unit
   static constexpr int NT = WI * WJ * 64;
   static constexpr int MI = BI / WI / 32, NJ = BJ / WJ / 32;
@@ -72,11 +76,11 @@ struct Tile {
   }
 
   template <Order O, int B, int U>
-  static __device__ __forceinline__ void load(const Operand& o, int64_t r0, int64_t k0, int64_t kend, u32x4 (&v)[U]) {
+  static __device__ __forceinline__ void load(const Operand& o, int64_t r0, int64_t k0, int64_t kend, u32x4 (&v)[U], int first = 0) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       int r, k;
-      unit<O, B>(threadIdx.x + i * NT, r, k);
+      unit<O, B>(threadIdx.x + (first + i) * NT, r, k);
       const T* p = static_cast<const T*>(o.p) + (O == kAlongK ? (r0 + r) * o.ld + (k0 + k) : (k0 + k) * o.ld + (r0 + r));
       // elements of the unit inside the matrix
       const bool in = r0 + r < o.rows && k0 + k < kend;
@@ -96,35 +100,34 @@ struct Tile {
   }
 
   template <Order O, int B, int U>
-  static __device__ __forceinline__ void store(char* lds, const u32x4 (&v)[U]) {
+  static __device__ __forceinline__ void store(uint32_t lds, const u32x4 (&v)[U], int first = 0) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       int r, k;
-      unit<O, B>(threadIdx.x + i * NT, r, k);
-      char* p = lds + at<O, B>(r, k);
+      unit<O, B>(threadIdx.x + (first + i) * NT, r, k);
+      const uint32_t p = lds + at<O, B>(r, k);
       if constexpr (P == 1) {
-        *reinterpret_cast<u32x4*>(p) = v[i];
+        *lds_at<u32x4>(p) = v[i];
       } else {
         uint32_t a[P], b[P];
         split2<P>(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]), a);
         split2<P>(__uint_as_float(v[i][2]), __uint_as_float(v[i][3]), b);
 #pragma unroll
-        for (int s = 0; s < P; ++s) *reinterpret_cast<u32x2*>(p + s * (B * BK * 2)) = (u32x2){a[s], b[s]};
+        for (int s = 0; s < P; ++s) *lds_at<u32x2>(p + s * (B * BK * 2)) = (u32x2){a[s], b[s]};
       }
     }
   }
 
   // 8 consecutive k of row r (this lane's 8 of the 16 of step ks)
   template <Order O, int B>
-  static __device__ __forceinline__ bf16x8 frag(const char* lds, int base, int ks, int lane) {
+  static __device__ __forceinline__ bf16x8 frag(uint32_t lds, int base, int ks, int lane) {
     if constexpr (O == kAlongK) {
-      return *reinterpret_cast<const bf16x8*>(lds + at<O, B>(base + (lane & 31), ks * 16 + (lane >> 5) * 8));
+      return *lds_at<const bf16x8>(lds + at<O, B>(base + (lane & 31), ks * 16 + (lane >> 5) * 8));
     } else {
       // 16 lanes read 4 lines of 16 rows and get 4 k of one row each
-      typedef __attribute__((address_space(3))) s16x4 Lds;
       const int k = ks * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2), r = base + (lane & 16) + (lane & 3) * 4;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(lds + at<O, B>(r, k)));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(lds + at<O, B>(r, k + 4)));
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(lds + at<O, B>(r, k)));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(lds + at<O, B>(r, k + 4)));
       typedef short s16x8 __attribute__((ext_vector_type(8)));
       return __builtin_bit_cast(bf16x8, (s16x8){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
     }
@@ -133,7 +136,7 @@ struct Tile {
   // acc[mi][nj][r]: row i = base_i + 32 mi + 8 (r / 4) + 4 (lane / 32) + r % 4,
   // column j = base_j + 32 nj + lane % 32
   static __device__ __forceinline__ void product(const Operand& X, const Operand& Y, int64_t i0, int64_t j0, int64_t k0,
-                                                 int64_t kend, char* lds, Acc& acc) {
+                                                 int64_t kend, uint32_t lds, Acc& acc) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int bi = (wave / WJ) * 32 * MI, bj = (wave % WJ) * 32 * NJ;
     u32x4 xv[XU], yv[YU];
@@ -145,7 +148,7 @@ struct Tile {
         for (int r = 0; r < 16; ++r) acc[mi][nj][r] = 0.0f;
     load<OX, BI>(X, i0, k0, kend, xv);
     load<OY, BJ>(Y, j0, k0, kend, yv);
-    char* buf = lds;
+    uint32_t buf = lds;
     for (int64_t k = k0; k < kend; k += BK) {
       store<OX, BI>(buf, xv);
       store<OY, BJ>(buf + P * XB, yv);
@@ -180,6 +183,198 @@ struct Tile {
   }
 };
 
+// The tile of large bf16 products: 256 x 256 results of four wavefronts, 128 x
+// 128 each, one to a SIMD with its sums in the accumulation registers.  LDS
+// reads are then half of what the matrix cores take the time for (64 KB of
+// reads and 32 KB of writes per 32 k against 1024 cycles of 128 bytes), where
+// eight wavefronts of 128 x 64 would need all of it.  Steps of 32 k go from
+// memory straight to LDS through four buffers, three steps ahead.  A step's only
+// barrier stands between its two halves, when the second half's operands are in
+// registers; reads and transfers are issued between products, a few at a time,
+// since a wavefront waits where the memory pipeline's queue is full.
+// STAGED_X / STAGED_Y: an operand whose rows are not whole 16-byte units goes
+// through registers instead.
+template <Order OX, Order OY, bool STAGED_X, bool STAGED_Y>
+struct BigTile {
+  static constexpr int BI = 256, BJ = 256, BK = 32, WI = 2, WJ = 2, MI = 4, NJ = 4, NT = 256;
+  static constexpr int BUFFERS = 4;
+  static constexpr uint32_t OPB = 256 * BK * 2, STAGE = 2 * OPB, LDS = BUFFERS * STAGE;   // bytes of an operand's step, of a step, of all
+  static constexpr int U = 4;                                     // 16-byte units per thread, operand and step
+  typedef f32x16 Acc[MI][NJ];
+  typedef Tile<Bf16, OX, OY, 256, 256, 2, 2, BK> Small;           // the LDS layout and guarded loads are its
+
+  // byte offset of this lane's unit of transfer q from the step's origin; the
+  // transfer fills 1 KB of LDS in lane order, so the lane fetches what the
+  // layout has in its place.  Units past the matrix repeat its last ones: they
+  // reach only results that are not written.
+  template <Order O>
+  static __device__ __forceinline__ uint32_t offset(const Operand& o, int64_t r0, int q) {
+    const int lane = threadIdx.x & 63, block = (threadIdx.x >> 6) * U + q;
+    if constexpr (O == kAlongK) {
+      int64_t r = block * 16 + (lane >> 2);
+      const int k = ((lane & 3) ^ ((r >> 2) & 3)) * 8;
+      if (r > o.rows - 1 - r0) r = o.rows - 1 - r0;
+      return (uint32_t)((r * o.ld + k) * 2);
+    } else {
+      const int k = block * 2 + (lane >> 5);
+      int64_t r = ((((lane & 31) >> 2) ^ (k & 3)) * 4 + (lane & 3)) * 8;
+      if (r > o.pad - 8 - r0) r = o.pad - 8 - r0;
+      return (uint32_t)((k * o.ld + r) * 2);
+    }
+  }
+
+  // 16 bytes a lane from base + off to LDS, 1 KB from `to` on (uniform)
+  static __device__ __forceinline__ void transfer(const void* base, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+  }
+
+  template <Order O, bool STAGED, int B>
+  struct Stream {
+    const char* base;       // the next step's origin
+    int64_t step;           // bytes from a step to the next
+    uint32_t to;            // this wavefront's part of a buffer
+    uint32_t off[STAGED ? 1 : U];
+    u32x4 held[STAGED ? U : 1];
+
+    __device__ __forceinline__ void init(const Operand& o, int64_t r0, int64_t k0, uint32_t lds) {
+      base = static_cast<const char*>(o.p) + (O == kAlongK ? r0 * o.ld + k0 : k0 * o.ld + r0) * 2;
+      step = (O == kAlongK ? (int64_t)BK : BK * o.ld) * 2;
+      to = __builtin_amdgcn_readfirstlane(lds + (threadIdx.x >> 6) * (U * 1024));
+      if constexpr (!STAGED) {
+#pragma unroll
+        for (int q = 0; q < U; ++q) off[q] = offset<O>(o, r0, q);
+      }
+    }
+    // transfer q of the next step, into the buffer at `at`; the last one moves on
+    __device__ __forceinline__ void send(int q, uint32_t at) {
+      transfer(base, off[q], to + at + q * 1024);
+      if (q == U - 1) base += step;
+    }
+  };
+
+  static __device__ __forceinline__ void product(const Operand& X, const Operand& Y, int64_t i0, int64_t j0, int64_t k0,
+                                                 int64_t kend, uint32_t lds, Acc& acc) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int bi = (wave / WJ) * 128, bj = (wave % WJ) * 128;
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+      for (int nj = 0; nj < NJ; ++nj)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[mi][nj][r] = 0.0f;
+    const int steps = k0 < kend ? (int)((kend - k0) / BK) : 0;   // whole steps
+    Stream<OX, STAGED_X, 256> sx;
+    Stream<OY, STAGED_Y, 256> sy;
+    sx.init(X, i0, k0, lds);
+    sy.init(Y, j0, k0, lds + OPB);
+    auto send = [&](int s, int n) {   // transfer n = 0..7 of step s
+      const uint32_t at = (uint32_t)(s % BUFFERS) * STAGE;
+      if (n < U) {
+        if constexpr (!STAGED_X) sx.send(n, at);
+      } else {
+        if constexpr (!STAGED_Y) sy.send(n - U, at);
+      }
+    };
+    auto fetch = [&](int s) {
+      if constexpr (STAGED_X) Small::template load<OX, 256, U>(X, i0, k0 + (int64_t)s * BK, kend, sx.held);
+      if constexpr (STAGED_Y) Small::template load<OY, 256, U>(Y, j0, k0 + (int64_t)s * BK, kend, sy.held);
+    };
+    auto put = [&](int s) {
+      const uint32_t b = lds + (uint32_t)(s % BUFFERS) * STAGE;
+      if constexpr (STAGED_X) Small::template store<OX, 256, U>(b, sx.held);
+      if constexpr (STAGED_Y) Small::template store<OY, 256, U>(b + OPB, sy.held);
+    };
+    bf16x8 x[2][MI], y[2][NJ];
+    auto read = [&](uint32_t b, int ks, int to, int n) {   // operand n = 0..7, in the order the products need them
+      if (n == 0 || n > NJ) x[to][n == 0 ? 0 : n - NJ] = Small::template frag<OX, 256>(b, bi + 32 * (n == 0 ? 0 : n - NJ), ks, lane);
+      else y[to][n - 1] = Small::template frag<OY, 256>(b + OPB, bj + 32 * (n - 1), ks, lane);
+    };
+    // the 16 products of one half step, the next half's reads behind the first
+    // 8 of them and 4 transfers behind the others
+    auto half = [&](int from, uint32_t b, int ks, int s, int first, bool more) {
+#pragma unroll
+      for (int n = 0; n < MI * NJ; ++n) {
+        if (n < 8) read(b, ks, from ^ 1, n);
+        else if (more && (n & 1) == 0) send(s, first + (n - 8) / 2);
+        __builtin_amdgcn_sched_barrier(0);
+        acc[n / NJ][n % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[from][n / NJ], y[from][n % NJ], acc[n / NJ][n % NJ], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    constexpr bool kStaged = STAGED_X || STAGED_Y;
+    if (steps > 0) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if (s < steps) {
+          if constexpr (kStaged) {
+            fetch(s);
+            put(s);
+          }
+#pragma unroll
+          for (int n = 0; n < (s < 3 ? 8 : 4); ++n) send(s, n);
+        }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      lds_only_barrier();
+#pragma unroll
+      for (int n = 0; n < 8; ++n) read(lds, 0, 0, n);
+      // ALL: this step has four more behind it, so that every transfer is there to make
+      auto step = [&](int s, auto all) {
+        constexpr bool ALL = decltype(all)::value;
+        const uint32_t b = lds + (uint32_t)(s % BUFFERS) * STAGE;
+        if constexpr (kStaged) {
+          if (ALL || s + 4 < steps) fetch(s + 4);
+        }
+        half(0, b, 1, s + 3, 4, ALL || s + 3 < steps);
+        // every read of this buffer has arrived, and the next step's transfers
+        // have landed: at most those of the two steps after it are on their way
+        if constexpr (ALL && !kStaged) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+        else if constexpr (ALL) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_only_barrier();
+        if constexpr (kStaged) {
+          if (ALL || s + 4 < steps) put(s + 4);
+        }
+        // (past the last step: reads of what is there, unused)
+        half(1, lds + (uint32_t)((s + 1) % BUFFERS) * STAGE, 0, s + 4, 0, ALL || s + 4 < steps);
+      };
+      int s = 0;
+      for (; s + 4 < steps; ++s) step(s, std::true_type{});
+      for (; s < steps; ++s) step(s, std::false_type{});
+      __syncthreads();
+    }
+    if (k0 + (int64_t)steps * BK < kend) {   // the last, partial step
+      u32x4 v[U];
+      Small::template load<OX, 256, U>(X, i0, k0 + (int64_t)steps * BK, kend, v);
+      Small::template store<OX, 256, U>(lds, v);
+      Small::template load<OY, 256, U>(Y, j0, k0 + (int64_t)steps * BK, kend, v);
+      Small::template store<OY, 256, U>(lds + OPB, v);
+      __syncthreads();
+      for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+        for (int n = 0; n < 8; ++n) read(lds, ks, 0, n);
+#pragma unroll
+        for (int n = 0; n < MI * NJ; ++n)
+          acc[n / NJ][n % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[0][n / NJ], y[0][n % NJ], acc[n / NJ][n % NJ], 0, 0, 0);
+      }
+      __syncthreads();
+    }
+  }
+};
+
+// Which tile a workgroup takes.  Neighbouring workgroups go to different XCDs,
+// each with its own L2, so each XCD gets a run of tiles of its own; in a run, up
+// to 8 columns of tiles are taken together, all their rows of tiles in turn, so
+// that what runs at once on an XCD shares both operands.
+__device__ __forceinline__ void tile_of(uint32_t block, int64_t itiles, int64_t jtiles, int64_t& it, int64_t& jt) {
+  constexpr uint32_t kXcds = 8, kCols = 8;
+  const uint32_t all = (uint32_t)(itiles * jtiles), per = all / kXcds, more = all % kXcds;
+  const uint32_t xcd = block % kXcds, t = xcd * per + (xcd < more ? xcd : more) + block / kXcds;
+  const uint32_t rows = (uint32_t)itiles, group = t / (kCols * rows), in = t % (kCols * rows);
+  const uint32_t left = (uint32_t)jtiles - group * kCols, cols = left < kCols ? left : kCols;
+  it = __builtin_amdgcn_readfirstlane(in / cols);   // (the same in every lane: kept in scalar registers)
+  jt = __builtin_amdgcn_readfirstlane(group * kCols + in % cols);
+}
+
 constexpr float kLog2e = 1.44269504088896341f;
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 // what maxima are subtracted from: a row without a finite logit subtracts 0
@@ -199,51 +394,78 @@ struct XArgs {
   int64_t itiles, jtiles;
 };
 
-// z of accumulator (mi, nj, r), -inf past the last output
+// row of accumulator entry r inside its 32 x 32 block
+__device__ __forceinline__ int entry_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
+// logits of this wavefront's blocks from output i0 on: the bias added, -inf past the last output
 template <class Tl>
 __device__ __forceinline__ void add_bias(typename Tl::Acc& acc, const float* bias, int64_t i0, int64_t M) {
   const int lane = threadIdx.x & 63;
+  const int left = M - i0 < Tl::BI ? (int)(M - i0) : Tl::BI;   // outputs from i0 on (negative: none)
+  if (bias && left >= 32 * Tl::MI) {
+    const float* b = bias + i0;
 #pragma unroll
-  for (int mi = 0; mi < Tl::MI; ++mi)
+    for (int mi = 0; mi < Tl::MI; ++mi)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int64_t i = i0 + 32 * mi + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-      const float b = i >= M ? -__builtin_inff() : bias ? bias[i] : 0.0f;
+      for (int r = 0; r < 16; ++r) {
+        const float v = b[32 * mi + entry_row(r, lane)];
 #pragma unroll
-      for (int nj = 0; nj < Tl::NJ; ++nj) acc[mi][nj][r] = i >= M ? b : acc[mi][nj][r] + b;
-    }
+        for (int nj = 0; nj < Tl::NJ; ++nj) acc[mi][nj][r] += v;
+      }
+  } else if (left < 32 * Tl::MI) {
+#pragma unroll
+    for (int mi = 0; mi < Tl::MI; ++mi)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i = 32 * mi + entry_row(r, lane);
+        const float v = i < left && bias ? bias[i0 + i] : 0.0f;
+#pragma unroll
+        for (int nj = 0; nj < Tl::NJ; ++nj) acc[mi][nj][r] = i < left ? acc[mi][nj][r] + v : -__builtin_inff();
+      }
+  }
 }
 
-template <class T, Order OW, int BI, int BJ, int WI, int WJ>
-__global__ void __launch_bounds__(WI * WJ * 64) xent_tile_kernel(XArgs a) {
-  typedef Tile<T, OW, kAlongK, BI, BJ, WI, WJ> Tl;
+// where a row's target lies from output i0 on; out of every tile for rows without one
+__device__ __forceinline__ int target_at(int64_t t, int64_t M, int64_t i0) {
+  const int64_t d = t - i0;
+  return t < 0 || t >= M || d < 0 || d >= (1 << 20) ? -1 : (int)d;
+}
+
+template <class T, class Tl>
+__global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
+  constexpr int BI = Tl::BI, BJ = Tl::BJ, WI = Tl::WI, WJ = Tl::WJ;
   extern __shared__ __align__(16) char lds[];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t jt = blockIdx.x % a.jtiles, it = blockIdx.x / a.jtiles;
+  int64_t it, jt;
+  tile_of(blockIdx.x, a.itiles, a.jtiles, it, jt);
   const int64_t i0 = it * BI, j0 = jt * BJ;
   typename Tl::Acc acc;
-  Tl::product(a.W, a.A, i0, j0, 0, a.D, lds, acc);
+  Tl::product(a.W, a.A, i0, j0, 0, a.D, lds_address(lds), acc);
   const int bi = (wave / WJ) * 32 * Tl::MI, bj = (wave % WJ) * 32 * Tl::NJ;
   add_bias<Tl>(acc, a.bias, i0 + bi, a.M);
   float2* red = reinterpret_cast<float2*>(lds);   // [WI][BJ]
 #pragma unroll
   for (int nj = 0; nj < Tl::NJ; ++nj) {
     const int64_t j = j0 + bj + 32 * nj + (lane & 31);
-    const int64_t t = j < a.N ? a.target[j] : -1;
+    const int t = j < a.N ? target_at(a.target[j], a.M, i0 + bi) : -1;
     float top = -__builtin_inff();
 #pragma unroll
-    for (int mi = 0; mi < Tl::MI; ++mi)
+    for (int mi = 0; mi < Tl::MI; ++mi) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        top = __builtin_fmaxf(top, acc[mi][nj][r]);
-        if (t == i0 + bi + 32 * mi + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3) && t < a.M) a.zt[j] = acc[mi][nj][r];
+      for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, acc[mi][nj][r]);
+      if (__any(t >= 32 * mi && t < 32 * mi + 32)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (t == 32 * mi + entry_row(r, lane)) a.zt[j] = acc[mi][nj][r];
       }
+    }
     top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+    const float base = base_of(top);
     float sum = 0.0f;
 #pragma unroll
     for (int mi = 0; mi < Tl::MI; ++mi)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sum += exp_of(acc[mi][nj][r] - base_of(top));
+      for (int r = 0; r < 16; ++r) sum += exp_of(acc[mi][nj][r] - base);
     sum += __shfl_xor(sum, 32);
     if (lane < 32) red[(wave / WJ) * BJ + bj + 32 * nj + lane] = make_float2(top, sum);
   }
@@ -284,44 +506,143 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2* part, cons
   }
 }
 
+// Writes a tile's results as bf16 or fp32: out[j][i], i contiguous, of I x J
+// results from the tile's own corner on.  bf16 goes through LDS (which is
+// free), so that every row is written in whole 16-byte units by neighbouring
+// lanes; a row's units are permuted by the row, so that 32 rows written at once
+// go to different banks.  fp32 goes out in the units the lanes hold.
+template <class T, class Tl>
+__device__ __forceinline__ void write_tile(typename Tl::Acc& acc, char* lds, T* out, int64_t ldo, int64_t I, int64_t J) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int bi = (wave / Tl::WJ) * 32 * Tl::MI, bj = (wave % Tl::WJ) * 32 * Tl::NJ;
+  if constexpr (sizeof(T) == 2) {
+    constexpr int C = Tl::BI / 8;   // units of a row
+    static_assert(Tl::BI * Tl::BJ * 2 <= Tl::LDS, "tile");
+#pragma unroll
+    for (int nj = 0; nj < Tl::NJ; ++nj) {
+      const int j = bj + 32 * nj + (lane & 31);
+#pragma unroll
+      for (int mi = 0; mi < Tl::MI; ++mi)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x2 lo = {acc[mi][nj][4 * q], acc[mi][nj][4 * q + 1]}, hi = {acc[mi][nj][4 * q + 2], acc[mi][nj][4 * q + 3]};
+          const int c = (bi + 32 * mi) / 8 + q;
+          *reinterpret_cast<u32x2*>(lds + j * (C * 16) + ((c ^ (j & (C - 1))) << 4) + (lane >> 5) * 8) =
+              (u32x2){__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)), __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
+        }
+    }
+    __syncthreads();
+    for (int u = threadIdx.x; u < Tl::BJ * C; u += Tl::NT) {
+      const int j = u / C, c = u % C;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(lds + j * (C * 16) + ((c ^ (j & (C - 1))) << 4));
+      if (j >= J) continue;
+      T* p = out + j * ldo + c * 8;
+      if (c * 8 + 8 <= I) {
+        store16(p, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c * 8 + e < I) p[e] = T{(uint16_t)(v[e >> 1] >> (16 * (e & 1)))};
+      }
+    }
+  } else {
+#pragma unroll
+    for (int nj = 0; nj < Tl::NJ; ++nj) {
+      const int j = bj + 32 * nj + (lane & 31);
+      if (j >= J) continue;
+#pragma unroll
+      for (int mi = 0; mi < Tl::MI; ++mi)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int i = bi + 32 * mi + 8 * q + 4 * (lane >> 5);
+          T* p = out + j * ldo + i;
+          if (i + 4 <= I) {
+            store16(p, __builtin_bit_cast(u32x4, (f32x4){acc[mi][nj][4 * q], acc[mi][nj][4 * q + 1], acc[mi][nj][4 * q + 2], acc[mi][nj][4 * q + 3]}));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (i + e < I) p[e] = acc[mi][nj][4 * q + e];
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+  }
+}
+
+// Adds what a tile of 32-bit sums (as write_tile writes them) holds.
+template <class Tl>
+__device__ __forceinline__ void add_tile(typename Tl::Acc& acc, const float* sum, int64_t ld, int64_t I, int64_t J) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int bi = (wave / Tl::WJ) * 32 * Tl::MI, bj = (wave % Tl::WJ) * 32 * Tl::NJ;
+#pragma unroll
+  for (int nj = 0; nj < Tl::NJ; ++nj) {
+    const int j = bj + 32 * nj + (lane & 31);
+#pragma unroll
+    for (int mi = 0; mi < Tl::MI; ++mi) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int i = bi + 32 * mi + 8 * q + 4 * (lane >> 5);
+        const float* p = sum + j * ld + i;
+        f32x4 v = {0, 0, 0, 0};
+        if (j < J) {
+          if (i + 4 <= I) {
+            v = __builtin_bit_cast(f32x4, load16(p));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (i + e < I) v[e] = p[e];
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[mi][nj][4 * q + e] += v[e];
+      }
+      __builtin_amdgcn_sched_barrier(0);   // (a few loads at a time: few registers)
+    }
+  }
+}
+
+// sum over the 32 lanes of a half wavefront, in every lane of it
+__device__ __forceinline__ float sum32(float v) {
+  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x121, 0xf, 0xf, false));   // rotate 16 lanes by 1
+  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x122, 0xf, 0xf, false));   // by 2
+  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x124, 0xf, 0xf, false));   // by 4
+  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, false));   // by 8
+  return v + __shfl_xor(v, 16);
+}
+
 // A tile of G: outputs m0 + i, rows j.
-template <class T, Order OW, int BI, int BJ, int WI, int WJ>
-__global__ void __launch_bounds__(WI * WJ * 64) xent_dz_kernel(XArgs a) {
-  typedef Tile<T, OW, kAlongK, BI, BJ, WI, WJ> Tl;
+template <class T, class Tl>
+__global__ void __launch_bounds__(Tl::NT, 1) xent_dz_kernel(XArgs a) {
+  constexpr int BI = Tl::BI, BJ = Tl::BJ, WJ = Tl::WJ;
   extern __shared__ __align__(16) char lds[];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t jt = blockIdx.x % a.jtiles, it = blockIdx.x / a.jtiles;
+  int64_t it, jt;
+  tile_of(blockIdx.x, a.itiles, a.jtiles, it, jt);
   const int64_t i0 = a.m0 + it * BI, j0 = jt * BJ;
   typename Tl::Acc acc;
-  Tl::product(a.W, a.A, i0, j0, 0, a.D, lds, acc);
+  Tl::product(a.W, a.A, i0, j0, 0, a.D, lds_address(lds), acc);
   const int bi = (wave / WJ) * 32 * Tl::MI, bj = (wave % WJ) * 32 * Tl::NJ;
   add_bias<Tl>(acc, a.bias, i0 + bi, a.M);
 #pragma unroll
   for (int nj = 0; nj < Tl::NJ; ++nj) {
     const int64_t j = j0 + bj + 32 * nj + (lane & 31);
-    const int64_t t = j < a.N ? a.target[j] : -1;
+    const int64_t target = j < a.N ? a.target[j] : -1;
     const float l = j < a.N ? a.lse[j] : 0.0f;
-    const bool live = t >= 0 && t < a.M && l != -__builtin_inff();
+    const bool live = target >= 0 && target < a.M && l != -__builtin_inff();
     const float g = live ? a.gloss[j] : 0.0f;
+    const int t = live ? target_at(target, a.M, i0 + bi) : -1;
 #pragma unroll
-    for (int mi = 0; mi < Tl::MI; ++mi)
+    for (int mi = 0; mi < Tl::MI; ++mi) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t i = i0 + bi + 32 * mi + 8 * q + 4 * (lane >> 5);
-        T out[4];
+      for (int r = 0; r < 16; ++r) acc[mi][nj][r] = exp_of(acc[mi][nj][r] - l);
+      if (__any(t >= 32 * mi && t < 32 * mi + 32)) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float v = exp_of(acc[mi][nj][4 * q + r] - l) - (t == i + r ? 1.0f : 0.0f);
-          v = live ? v * g : 0.0f;
-          acc[mi][nj][4 * q + r] = v;
-          out[r] = from_float<T>(v);
-        }
-        if (j < a.N && i - a.m0 < a.ldz) {   // (ldz is a multiple of 64)
-          T* p = static_cast<T*>(a.dz) + j * a.ldz + (i - a.m0);
-          if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(p) = *reinterpret_cast<const u32x2*>(out);
-          else *reinterpret_cast<u32x4*>(p) = *reinterpret_cast<const u32x4*>(out);
-        }
+        for (int r = 0; r < 16; ++r)
+          if (t == 32 * mi + entry_row(r, lane)) acc[mi][nj][r] -= 1.0f;
       }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[mi][nj][r] = live ? acc[mi][nj][r] * g : 0.0f;
+    }
   }
   // sums over the tile's rows, for the bias gradient
   float* red = reinterpret_cast<float*>(lds);   // [WJ][BI]
@@ -332,9 +653,8 @@ __global__ void __launch_bounds__(WI * WJ * 64) xent_dz_kernel(XArgs a) {
       float s = acc[mi][0][r];
 #pragma unroll
       for (int nj = 1; nj < Tl::NJ; ++nj) s += acc[mi][nj][r];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) s += __shfl_xor(s, o);
-      if ((lane & 31) == 0) red[(wave % WJ) * BI + bi + 32 * mi + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)] = s;
+      s = sum32(s);
+      if ((lane & 31) == 0) red[(wave % WJ) * BI + bi + 32 * mi + entry_row(r, lane)] = s;
     }
   __syncthreads();
   for (int i = threadIdx.x; i < BI; i += Tl::NT) {
@@ -343,6 +663,8 @@ __global__ void __launch_bounds__(WI * WJ * 64) xent_dz_kernel(XArgs a) {
     for (int w = 1; w < WJ; ++w) s += red[w * BI + i];
     if (it * BI + i < a.ldz) a.cpart[jt * a.ldz + it * BI + i] = s;
   }
+  __syncthreads();
+  write_tile<T, Tl>(acc, lds, static_cast<T*>(a.dz) + j0 * a.ldz + it * BI, a.ldz, a.ldz - it * BI, a.N - j0);
 }
 
 __global__ void __launch_bounds__(256) xent_dbias_kernel(const float* cpart, int64_t jtiles, int64_t ldz, int64_t n, float* out) {
@@ -353,7 +675,7 @@ __global__ void __launch_bounds__(256) xent_dbias_kernel(const float* cpart, int
   }
 }
 
-// out[i][j] = sum_k X[i][k] Y[j][k], added to what `sum` holds where it is
+// out[j][i] = sum_k X[i][k] Y[j][k], added to what `sum` holds where it is
 // not the first piece; written to `sum` (32 bits) unless it is the last.
 // splits > 1: blockIdx.y takes its share of k and leaves it in part[split].
 struct GemmArgs {
@@ -361,47 +683,32 @@ struct GemmArgs {
   int64_t K;
   int64_t itiles, jtiles;
   void* out; int64_t ldo;
-  float* sum;               // [rows of X][rows of Y] or null
+  float* sum;               // [rows of Y][rows of X] or null
   int first, last;
   float* part; int splits; int64_t kper;
 };
 
-template <class T, Order OX, Order OY, int BI, int BJ, int WI, int WJ>
-__global__ void __launch_bounds__(WI * WJ * 64) xent_gemm_kernel(GemmArgs a) {
-  typedef Tile<T, OX, OY, BI, BJ, WI, WJ> Tl;
+enum GemmOut : int {
+  kOut,      // the result, one piece
+  kPart,     // 32-bit results: a share of k, or the first of several pieces
+  kMore,     // a further piece: added to the sum
+  kLast      // the last of several: the sum added, the result written
+};
+
+template <class T, class Tl, GemmOut MODE>
+__global__ void __launch_bounds__(Tl::NT, 1) xent_gemm_kernel(GemmArgs a) {
+  constexpr int BI = Tl::BI, BJ = Tl::BJ;
   extern __shared__ __align__(16) char lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t jt = blockIdx.x % a.jtiles, it = blockIdx.x / a.jtiles;
+  int64_t it, jt;
+  tile_of(blockIdx.x, a.itiles, a.jtiles, it, jt);
   const int64_t i0 = it * BI, j0 = jt * BJ, I = a.X.rows, J = a.Y.rows;
-  int64_t k0 = 0, kend = a.K;
-  if (a.splits > 1) {
-    k0 = blockIdx.y * a.kper;
-    kend = k0 + a.kper < a.K ? k0 + a.kper : a.K;
-  }
+  const int64_t k0 = blockIdx.y * a.kper, kend = k0 + a.kper < a.K ? k0 + a.kper : a.K;
   typename Tl::Acc acc;
-  Tl::product(a.X, a.Y, i0, j0, k0, kend, lds, acc);
-  const int bi = (wave / WJ) * 32 * Tl::MI, bj = (wave % WJ) * 32 * Tl::NJ;
-  float* part = a.splits > 1 ? a.part + blockIdx.y * I * J : nullptr;
-#pragma unroll
-  for (int mi = 0; mi < Tl::MI; ++mi)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int64_t i = i0 + bi + 32 * mi + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-#pragma unroll
-      for (int nj = 0; nj < Tl::NJ; ++nj) {
-        const int64_t j = j0 + bj + 32 * nj + (lane & 31);
-        if (i < I && j < J) {
-          float v = acc[mi][nj][r];
-          if (part) {
-            part[i * J + j] = v;
-          } else {
-            if (!a.first) v += a.sum[i * J + j];
-            if (a.last) static_cast<T*>(a.out)[i * a.ldo + j] = from_float<T>(v);
-            else a.sum[i * J + j] = v;
-          }
-        }
-      }
-    }
+  Tl::product(a.X, a.Y, i0, j0, k0, kend, lds_address(lds), acc);
+  float* sum = (a.splits > 1 ? a.part + blockIdx.y * I * J : a.sum) + j0 * I + i0;
+  if constexpr (MODE == kMore || MODE == kLast) add_tile<Tl>(acc, sum, I, I - i0, J - j0);
+  if constexpr (MODE == kOut || MODE == kLast) write_tile<T, Tl>(acc, lds, static_cast<T*>(a.out) + j0 * a.ldo + i0, a.ldo, I - i0, J - j0);
+  else write_tile<float, Tl>(acc, lds, sum, I, I - i0, J - j0);
 }
 
 // Joins the shares of a split product, in order.
@@ -411,7 +718,7 @@ __global__ void __launch_bounds__(256) xent_join_splits_kernel(GemmArgs a) {
   for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < I * J; e += (int64_t)gridDim.x * 256) {
     float v = a.first ? 0.0f : a.sum[e];
     for (int s = 0; s < a.splits; ++s) v += a.part[s * I * J + e];
-    if (a.last) static_cast<T*>(a.out)[e / J * a.ldo + e % J] = from_float<T>(v);
+    if (a.last) static_cast<T*>(a.out)[e / I * a.ldo + e % I] = from_float<T>(v);
     else a.sum[e] = v;
   }
 }
@@ -430,48 +737,6 @@ constexpr int64_t kMaxBlocks = (1ll << 31) - 1;
 constexpr int kWide = 128;   // outputs or columns of a tile
 constexpr int kSlots = 512;  // workgroups that fill the card: two to a compute unit
 
-// rows of a logits tile: the wide one where that leaves enough workgroups
-int row_tile(int64_t N, int64_t M) { return cdiv(N, kWide) * cdiv(M, kWide) >= 256 ? kWide : 32; }
-
-// Outputs per piece of the gradient: G of a piece stays within 128 MiB (half
-// of the memory-side cache), at least 256 outputs.
-int64_t piece(int64_t N, int64_t M, int64_t elem) {
-  int64_t p = (128ll << 20) / (N * elem) / 256 * 256;
-  if (p < 256) p = 256;
-  return p < up(M, 64) ? p : up(M, 64);
-}
-
-struct GradPlan {
-  int64_t p, jt;                 // outputs per piece, row tiles
-  int sa, sb;                    // shares of k of dA and dB
-  int64_t off_dz, off_c, off_sum, off_part, total;
-};
-
-int splits_for(int64_t tiles, int64_t K, int bk) {
-  int64_t s = kSlots / (tiles > 0 ? tiles : 1);
-  const int64_t most = K / (8 * bk);   // at least 8 steps each
-  if (s > most) s = most;
-  return s < 1 ? 1 : (int)(s > 64 ? 64 : s);
-}
-
-GradPlan grad_plan(int64_t N, int64_t D, int64_t M, int64_t elem, bool md) {
-  GradPlan g{};
-  const int bk = elem == 2 ? 64 : 32;
-  g.p = piece(N, M, elem);
-  g.jt = cdiv(N, row_tile(N, g.p));
-  g.sa = splits_for(cdiv(N, N <= 32 ? 32 : kWide) * cdiv(D, kWide), g.p, bk);
-  g.sb = splits_for(cdiv(D, kWide) * cdiv(g.p, kWide), N, bk);
-  int64_t off = 0;
-  auto take = [&](int64_t bytes) { const int64_t o = off; off += up(bytes, 256); return o; };
-  g.off_dz = take(N * g.p * elem);
-  g.off_c = take(g.jt * g.p * 4);
-  g.off_sum = take(g.p < M ? N * D * 4 : 0);
-  const int64_t pa = g.sa > 1 ? g.sa * N * D * 4 : 0, pb = g.sb > 1 ? g.sb * D * g.p * 4 : 0;
-  g.off_part = take(pa > pb ? pa : pb);
-  g.total = off > 256 ? off : 256;
-  return g;
-}
-
 template <class K, class Args>
 hipError_t launch(K kernel, int lds, int64_t blocks, int splits, int threads, const Args& a, hipStream_t stream) {
   if (blocks > kMaxBlocks) return hipErrorInvalidValue;
@@ -482,80 +747,162 @@ hipError_t launch(K kernel, int lds, int64_t blocks, int splits, int threads, co
   return hipGetLastError();
 }
 
-template <class T, Order OW, bool GRAD, int BI, int BJ, int WI, int WJ>
+template <class T, bool GRAD, class Tl>
 hipError_t launch_logits(XArgs& a, int64_t outputs, hipStream_t s) {
-  typedef Tile<T, OW, kAlongK, BI, BJ, WI, WJ> Tl;
-  a.itiles = cdiv(outputs, BI);
-  a.jtiles = cdiv(a.N, BJ);
-  if constexpr (GRAD) return launch(xent_dz_kernel<T, OW, BI, BJ, WI, WJ>, Tl::LDS, a.itiles * a.jtiles, 1, Tl::NT, a, s);
-  else return launch(xent_tile_kernel<T, OW, BI, BJ, WI, WJ>, Tl::LDS, a.itiles * a.jtiles, 1, Tl::NT, a, s);
+  a.itiles = cdiv(outputs, Tl::BI);
+  a.jtiles = cdiv(a.N, Tl::BJ);
+  if constexpr (GRAD) return launch(xent_dz_kernel<T, Tl>, Tl::LDS, a.itiles * a.jtiles, 1, Tl::NT, a, s);
+  else return launch(xent_tile_kernel<T, Tl>, Tl::LDS, a.itiles * a.jtiles, 1, Tl::NT, a, s);
+}
+
+// Whether an operand's rows are whole 16-byte units (and a step's offsets fit
+// in 32 bits), so that they can go straight to LDS.  along_i: its own index is
+// the contiguous one.
+bool direct(const Operand& o, bool along_i) {
+  return aligned(o.p, 16) && o.ld % 8 == 0 && (!along_i || o.pad % 8 == 0) && o.ld <= (1 << 22);
+}
+
+// Rows of a logits tile: 256 (large bf16 products with whole units in A), 128,
+// or 32 where the wider ones would leave compute units without work.
+template <class T>
+int row_tile(const XArgs& a, int64_t outputs) {
+  if (sizeof(T) == 2 && a.N >= 192 && direct(a.A, false) && cdiv(a.N, 256) * cdiv(outputs, 256) >= 192) return 256;
+  return cdiv(a.N, 128) * cdiv(outputs, 128) >= 256 ? 128 : 32;
 }
 
 template <class T, bool GRAD>
 hipError_t logits(XArgs& a, int64_t outputs, int rows, bool md, hipStream_t s) {
-  if (rows == kWide) return md ? launch_logits<T, kAlongK, GRAD, 128, 128, 2, 2>(a, outputs, s) : launch_logits<T, kAlongI, GRAD, 128, 128, 2, 2>(a, outputs, s);
-  return md ? launch_logits<T, kAlongK, GRAD, 128, 32, 4, 1>(a, outputs, s) : launch_logits<T, kAlongI, GRAD, 128, 32, 4, 1>(a, outputs, s);
+  if constexpr (sizeof(T) == 2) {
+    if (rows == 256) {
+      if (direct(a.W, !md)) return md ? launch_logits<T, GRAD, BigTile<kAlongK, kAlongK, false, false>>(a, outputs, s)
+                                 : launch_logits<T, GRAD, BigTile<kAlongI, kAlongK, false, false>>(a, outputs, s);
+      return md ? launch_logits<T, GRAD, BigTile<kAlongK, kAlongK, true, false>>(a, outputs, s)
+                : launch_logits<T, GRAD, BigTile<kAlongI, kAlongK, true, false>>(a, outputs, s);
+    }
+  }
+  if (rows >= 128) return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>>(a, outputs, s)
+                             : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 128, 2, 2>>(a, outputs, s);
+  return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 32, 4, 1>>(a, outputs, s)
+            : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 32, 4, 1>>(a, outputs, s);
 }
 
-template <class T, Order OX, Order OY, int BI, int BJ, int WI, int WJ>
-hipError_t gemm(GemmArgs a, hipStream_t s) {
-  typedef Tile<T, OX, OY, BI, BJ, WI, WJ> Tl;
-  a.itiles = cdiv(a.X.rows, BI);
-  a.jtiles = cdiv(a.Y.rows, BJ);
+// Shares of k for `tiles` tiles: workgroups for the whole card, at least 8 steps each.
+int splits_for(int64_t tiles, int64_t slots, int64_t K, int bk) {
+  int64_t s = slots / (tiles > 0 ? tiles : 1);
+  const int64_t most = K / (8 * bk);
+  if (s > most) s = most;
+  return s < 1 ? 1 : (int)(s > 64 ? 64 : s);
+}
+
+template <class T, class Tl, bool PIECES>
+hipError_t gemm(GemmArgs a, int64_t part_bytes, hipStream_t s) {
+  a.itiles = cdiv(a.X.rows, Tl::BI);
+  a.jtiles = cdiv(a.Y.rows, Tl::BJ);
+  a.splits = splits_for(a.itiles * a.jtiles, Tl::BI == 256 ? kSlots / 2 : kSlots, a.K, Tl::BK);
+  const int64_t fit = part_bytes / (a.X.rows * a.Y.rows * 4);
+  if (a.splits > fit) a.splits = fit < 1 ? 1 : (int)fit;
   a.kper = up(cdiv(a.K, a.splits), Tl::BK);
   a.splits = (int)cdiv(a.K, a.kper);
-  hipError_t e = launch(xent_gemm_kernel<T, OX, OY, BI, BJ, WI, WJ>, Tl::LDS, a.itiles * a.jtiles, a.splits, Tl::NT, a, s);
+  const GemmOut mode = a.splits > 1 || (a.first && !a.last) ? kPart : a.first ? kOut : a.last ? kLast : kMore;
+  hipError_t e;
+  if (mode == kOut) e = launch(xent_gemm_kernel<T, Tl, kOut>, Tl::LDS, a.itiles * a.jtiles, a.splits, Tl::NT, a, s);
+  else if (mode == kPart) e = launch(xent_gemm_kernel<T, Tl, kPart>, Tl::LDS, a.itiles * a.jtiles, a.splits, Tl::NT, a, s);
+  else if constexpr (PIECES) {
+    if (mode == kLast) e = launch(xent_gemm_kernel<T, Tl, kLast>, Tl::LDS, a.itiles * a.jtiles, a.splits, Tl::NT, a, s);
+    else e = launch(xent_gemm_kernel<T, Tl, kMore>, Tl::LDS, a.itiles * a.jtiles, a.splits, Tl::NT, a, s);
+  } else {
+    return hipErrorInvalidValue;
+  }
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t b = cdiv(a.X.rows * a.Y.rows, 256);
   hipLaunchKernelGGL((xent_join_splits_kernel<T>), dim3((unsigned)(b < 4096 ? b : 4096)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
+struct GradPlan {
+  int64_t p;                                    // outputs per piece
+  int64_t off_dz, off_c, off_sum, off_part, part, total;
+};
+
+// Outputs per piece of the gradient: G of a piece stays within 256 MiB, at least 256 outputs.
+GradPlan grad_plan(int64_t N, int64_t D, int64_t M, int64_t elem) {
+  GradPlan g{};
+  int64_t p = (256ll << 20) / (N * elem) / 256 * 256;
+  if (p < 256) p = 256;
+  g.p = p < up(M, 64) ? p : up(M, 64);
+  int64_t off = 0;
+  auto take = [&](int64_t bytes) { const int64_t o = off; off += up(bytes, 256); return o; };
+  g.off_dz = take(N * g.p * elem);
+  g.off_c = take(cdiv(N, 32) * g.p * 4);
+  g.off_sum = take(g.p < M ? N * D * 4 : 0);
+  // shares of a product: at most kSlots tiles of 128 x 128
+  g.part = (int64_t)kSlots * 128 * 128 * 4;
+  g.off_part = take(g.part);
+  g.total = off;
+  return g;
+}
+
 template <class T>
 hipError_t grad(XArgs a, bool md, void* dA, void* dB, float* dbias, char* ws, hipStream_t s) {
-  const GradPlan g = grad_plan(a.N, a.D, a.M, sizeof(T), md);
+  const GradPlan g = grad_plan(a.N, a.D, a.M, sizeof(T));
   a.dz = ws + g.off_dz;
   a.cpart = reinterpret_cast<float*>(ws + g.off_c);
   T* B = static_cast<T*>(const_cast<void*>(a.W.p));
   for (int64_t m0 = 0; m0 < a.M; m0 += g.p) {
     const int64_t n = a.M - m0 < g.p ? a.M - m0 : g.p;
-    a.m0 = m0;
-    a.ldz = up(n, 64);
-    hipError_t e = logits<T, true>(a, a.ldz, row_tile(a.N, g.p), md, s);
+    XArgs z = a;
+    z.m0 = m0;
+    z.ldz = up(n, 64);
+    hipError_t e = logits<T, true>(z, z.ldz, row_tile<T>(a, g.p), md, s);
     if (e != hipSuccess) return e;
     const int64_t b = cdiv(n, 256);
-    hipLaunchKernelGGL(xent_dbias_kernel, dim3((unsigned)(b < 4096 ? b : 4096)), dim3(256), 0, s, a.cpart, a.jtiles, a.ldz, n, dbias + m0);
+    hipLaunchKernelGGL(xent_dbias_kernel, dim3((unsigned)(b < 4096 ? b : 4096)), dim3(256), 0, s, z.cpart, z.jtiles, z.ldz, n, dbias + m0);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    const Operand zk{a.dz, a.ldz, a.N}, zi{a.dz, a.ldz, n};
+    const Operand zk{z.dz, z.ldz, a.N, a.N}, zi{z.dz, z.ldz, n, z.ldz};
     GemmArgs x{};
     x.sum = reinterpret_cast<float*>(ws + g.off_sum);
     x.part = reinterpret_cast<float*>(ws + g.off_part);
     // dA [N][D] += G B^T over the piece's outputs
-    x.X = zk;
-    x.Y = Operand{md ? B + m0 * a.W.ld : B + m0, a.W.ld, a.D};
+    x.X = Operand{md ? B + m0 * a.W.ld : B + m0, a.W.ld, a.D, a.D};
+    x.Y = zk;
     x.K = n;
     x.out = dA; x.ldo = a.D;
     x.first = m0 == 0; x.last = m0 + n == a.M;
-    x.splits = g.sa;
-    if (a.N <= 32) e = md ? gemm<T, kAlongK, kAlongI, 32, 128, 1, 4>(x, s) : gemm<T, kAlongK, kAlongK, 32, 128, 1, 4>(x, s);
-    else e = md ? gemm<T, kAlongK, kAlongI, 128, 128, 2, 2>(x, s) : gemm<T, kAlongK, kAlongK, 128, 128, 2, 2>(x, s);
+    bool done = false;
+    if constexpr (sizeof(T) == 2) {
+      if (a.N >= 256 && a.D >= 256) {
+        done = true;
+        if (direct(x.X, md)) e = md ? gemm<T, BigTile<kAlongI, kAlongK, false, false>, true>(x, g.part, s) : gemm<T, BigTile<kAlongK, kAlongK, false, false>, true>(x, g.part, s);
+        else e = md ? gemm<T, BigTile<kAlongI, kAlongK, true, false>, true>(x, g.part, s) : gemm<T, BigTile<kAlongK, kAlongK, true, false>, true>(x, g.part, s);
+      }
+    }
+    if (done) {}
+    else if (a.N <= 32) e = md ? gemm<T, Tile<T, kAlongI, kAlongK, 128, 32, 4, 1>, true>(x, g.part, s) : gemm<T, Tile<T, kAlongK, kAlongK, 128, 32, 4, 1>, true>(x, g.part, s);
+    else e = md ? gemm<T, Tile<T, kAlongI, kAlongK, 128, 128, 2, 2>, true>(x, g.part, s) : gemm<T, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>, true>(x, g.part, s);
     if (e != hipSuccess) return e;
     // dB = A^T G: [D][M] columns m0.., or [M][D] rows m0..
-    const Operand ai{a.A.p, a.A.ld, a.D};
-    x.X = md ? zi : ai;
-    x.Y = md ? ai : zi;
+    const Operand ai{a.A.p, a.A.ld, a.D, a.D};
+    x.X = md ? ai : zi;
+    x.Y = md ? zi : ai;
     x.K = a.N;
     x.out = static_cast<T*>(dB) + (md ? m0 * a.D : m0); x.ldo = md ? a.D : a.M;
     x.first = x.last = 1;
-    x.splits = g.sb;
-    if ((e = gemm<T, kAlongI, kAlongI, 128, 128, 2, 2>(x, s)) != hipSuccess) return e;
+    done = false;
+    if constexpr (sizeof(T) == 2) {
+      if (direct(ai, true) && cdiv(a.D, 256) * cdiv(n, 256) >= 192) {
+        done = true;
+        e = gemm<T, BigTile<kAlongI, kAlongI, false, false>, false>(x, g.part, s);
+      }
+    }
+    if (!done) e = gemm<T, Tile<T, kAlongI, kAlongI, 128, 128, 2, 2>, false>(x, g.part, s);
+    if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
 template <class T>
 hipError_t forward(XArgs a, bool md, float* loss, float* lse, hipStream_t s) {
-  hipError_t e = logits<T, false>(a, a.M, row_tile(a.N, a.M), md, s);
+  hipError_t e = logits<T, false>(a, a.M, row_tile<T>(a, a.M), md, s);
   if (e != hipSuccess) return e;
   const int64_t b = cdiv(a.N, 4);
   hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)(b < 65536 ? b : 65536)), dim3(256), 0, s, a.part, a.zt, a.target, a.N, a.M,
@@ -576,8 +923,8 @@ int check(const void* A, int32_t dtype, int64_t N, int32_t D, int64_t lda, const
 XArgs args(const void* A, int64_t N, int32_t D, int64_t lda, const void* B, int32_t M, int32_t outputs_first,
            const float* col_bias, const int64_t* target) {
   XArgs a{};
-  a.W = Operand{B, outputs_first ? D : M, M};
-  a.A = Operand{A, lda, N};
+  a.W = Operand{B, outputs_first ? D : M, M, M};
+  a.A = Operand{A, lda, N, N};
   a.N = N; a.D = D; a.M = M;
   a.bias = col_bias; a.target = target;
   return a;
@@ -617,7 +964,7 @@ int maddness_linear_xent(const void* A, int32_t dtype, int64_t N, int32_t D, int
 int64_t maddness_linear_xent_grad_workspace_bytes(int64_t N, int32_t D, int32_t M, int32_t dtype) {
   if (N < 0 || N >= kMaxN || D <= 0 || M <= 0 || (dtype != MADDNESS_F32 && dtype != MADDNESS_BF16)) return -1;
   if (N == 0) return 256;
-  return grad_plan(N, D, M, dtype == MADDNESS_F32 ? 4 : 2, false).total;
+  return grad_plan(N, D, M, dtype == MADDNESS_F32 ? 4 : 2).total;
 }
 
 int maddness_linear_xent_grad(const void* A, int32_t dtype, int64_t N, int32_t D, int64_t lda, const void* B, int32_t M,

@@ -62,6 +62,15 @@ __device__ __forceinline__ u32x4 load16(const void* p) {
   return (u32x4){v.w[0], v.w[1], v.w[2], v.w[3]};
 }
 
+__device__ __forceinline__ void store16(void* p, u32x4 v) { *static_cast<Bytes16*>(p) = Bytes16{{v[0], v[1], v[2], v[3]}}; }
+
+// LDS by byte address
+template <class V> using LdsPtr = __attribute__((address_space(3))) V*;
+template <class V> __device__ __forceinline__ LdsPtr<V> lds_at(uint32_t byte) { return (LdsPtr<V>)(uintptr_t)byte; }
+__device__ __forceinline__ uint32_t lds_address(const void* p) {   // (uniform)
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LdsPtr<const char>)p);
+}
+
 // A barrier that orders LDS only: global loads stay in flight across it.
 __device__ __forceinline__ void lds_only_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
