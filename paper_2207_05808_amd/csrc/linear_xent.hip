@@ -397,32 +397,25 @@ struct XArgs {
 // row of accumulator entry r inside its 32 x 32 block
 __device__ __forceinline__ int entry_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 
-// logits of this wavefront's blocks from output i0 on: the bias added, -inf past the last output
+// What is added to a wavefront's products, whose outputs begin at i0: the bias
+// of each, -inf past the last output.
 template <class Tl>
-__device__ __forceinline__ void add_bias(typename Tl::Acc& acc, const float* bias, int64_t i0, int64_t M) {
+__device__ __forceinline__ void load_bias(float (&b)[Tl::MI][16], const float* bias, int64_t i0, int64_t M) {
   const int lane = threadIdx.x & 63;
-  const int left = M - i0 < Tl::BI ? (int)(M - i0) : Tl::BI;   // outputs from i0 on (negative: none)
-  if (bias && left >= 32 * Tl::MI) {
-    const float* b = bias + i0;
 #pragma unroll
-    for (int mi = 0; mi < Tl::MI; ++mi)
+  for (int mi = 0; mi < Tl::MI; ++mi)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float v = b[32 * mi + entry_row(r, lane)];
+    for (int q = 0; q < 4; ++q) {
+      const int64_t i = i0 + 32 * mi + entry_row(4 * q, lane);
+      if (i + 4 <= M) {
+        const f32x4 v = bias ? __builtin_bit_cast(f32x4, load16(bias + i)) : (f32x4){0, 0, 0, 0};
 #pragma unroll
-        for (int nj = 0; nj < Tl::NJ; ++nj) acc[mi][nj][r] += v;
+        for (int e = 0; e < 4; ++e) b[mi][4 * q + e] = v[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[mi][4 * q + e] = i + e >= M ? -__builtin_inff() : bias ? bias[i + e] : 0.0f;
       }
-  } else if (left < 32 * Tl::MI) {
-#pragma unroll
-    for (int mi = 0; mi < Tl::MI; ++mi)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int i = 32 * mi + entry_row(r, lane);
-        const float v = i < left && bias ? bias[i0 + i] : 0.0f;
-#pragma unroll
-        for (int nj = 0; nj < Tl::NJ; ++nj) acc[mi][nj][r] = i < left ? acc[mi][nj][r] + v : -__builtin_inff();
-      }
-  }
+    }
 }
 
 // where a row's target lies from output i0 on; out of every tile for rows without one
@@ -442,7 +435,8 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
   typename Tl::Acc acc;
   Tl::product(a.W, a.A, i0, j0, 0, a.D, lds_address(lds), acc);
   const int bi = (wave / WJ) * 32 * Tl::MI, bj = (wave % WJ) * 32 * Tl::NJ;
-  add_bias<Tl>(acc, a.bias, i0 + bi, a.M);
+  float b[Tl::MI][16];
+  load_bias<Tl>(b, a.bias, i0 + bi, a.M);
   float2* red = reinterpret_cast<float2*>(lds);   // [WI][BJ]
 #pragma unroll
   for (int nj = 0; nj < Tl::NJ; ++nj) {
@@ -452,11 +446,12 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
 #pragma unroll
     for (int mi = 0; mi < Tl::MI; ++mi) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, acc[mi][nj][r]);
+      for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, acc[mi][nj][r] + b[mi][r]);
       if (__any(t >= 32 * mi && t < 32 * mi + 32)) {
+        asm volatile("");   // (a branch: seldom taken)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (t == 32 * mi + entry_row(r, lane)) a.zt[j] = acc[mi][nj][r];
+          if (t == 32 * mi + entry_row(r, lane)) a.zt[j] = acc[mi][nj][r] + b[mi][r];
       }
     }
     top = __builtin_fmaxf(top, __shfl_xor(top, 32));
@@ -465,7 +460,7 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
 #pragma unroll
     for (int mi = 0; mi < Tl::MI; ++mi)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sum += exp_of(acc[mi][nj][r] - base);
+      for (int r = 0; r < 16; ++r) sum += exp_of(acc[mi][nj][r] + b[mi][r] - base);
     sum += __shfl_xor(sum, 32);
     if (lane < 32) red[(wave / WJ) * BJ + bj + 32 * nj + lane] = make_float2(top, sum);
   }
@@ -506,66 +501,80 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2* part, cons
   }
 }
 
-// Writes a tile's results as bf16 or fp32: out[j][i], i contiguous, of I x J
-// results from the tile's own corner on.  bf16 goes through LDS (which is
-// free), so that every row is written in whole 16-byte units by neighbouring
-// lanes; a row's units are permuted by the row, so that 32 rows written at once
-// go to different banks.  fp32 goes out in the units the lanes hold.
+// A tile's results as bf16 on their way to memory, out[j][i] with i contiguous:
+// through LDS, so that every row is written in whole 16-byte units by
+// neighbouring lanes.  A row's units are permuted by the row, so that 32 rows
+// written at once go to different banks.
+template <class Tl>
+__device__ __forceinline__ void stage4(char* lds, int i, int j, float a, float b, float c, float d) {   // results i .. i + 3 of row j
+  constexpr int C = Tl::BI / 8;   // units of a row
+  static_assert(Tl::BI * Tl::BJ * 2 <= Tl::LDS, "tile");
+  *reinterpret_cast<u32x2*>(lds + j * (C * 16) + (((i >> 3) ^ (j & (C - 1))) << 4) + (i & 4) * 2) =
+      (u32x2){__builtin_bit_cast(uint32_t, __builtin_convertvector(((f32x2){a, b}), bf16x2)),
+              __builtin_bit_cast(uint32_t, __builtin_convertvector(((f32x2){c, d}), bf16x2))};
+}
+
+template <class Tl>
+__device__ __forceinline__ void write_staged(const char* lds, Bf16* out, int64_t ldo, int64_t I, int64_t J) {
+  constexpr int C = Tl::BI / 8, STEP = Tl::NT / C, BATCH = Tl::BJ / STEP < 8 ? Tl::BJ / STEP : 8;
+  const int c = threadIdx.x % C, left = I - c * 8 < 8 ? (int)(I - c * 8) : 8;
+  if (left <= 0) return;
+  for (int j0 = threadIdx.x / C; j0 < Tl::BJ; j0 += STEP * BATCH) {
+    u32x4 v[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int j = j0 + k * STEP;
+      v[k] = *reinterpret_cast<const u32x4*>(lds + j * (C * 16) + ((c ^ (j & (C - 1))) << 4));
+    }
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int j = j0 + k * STEP;
+      if (j >= J) break;
+      Bf16* p = out + j * ldo + c * 8;
+      if (left == 8) {
+        store16(p, v[k]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < left) p[e] = Bf16{(uint16_t)(v[k][e >> 1] >> (16 * (e & 1)))};
+      }
+    }
+  }
+}
+
+// fp32 results i .. i + 3 of a row, `left` of them inside the matrix
+__device__ __forceinline__ void write4(float* p, int64_t left, f32x4 v) {
+  if (left >= 4) {
+    store16(p, __builtin_bit_cast(u32x4, v));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < left) p[e] = v[e];
+  }
+}
+
+// A tile of I x J results from its own corner on.
 template <class T, class Tl>
 __device__ __forceinline__ void write_tile(typename Tl::Acc& acc, char* lds, T* out, int64_t ldo, int64_t I, int64_t J) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int bi = (wave / Tl::WJ) * 32 * Tl::MI, bj = (wave % Tl::WJ) * 32 * Tl::NJ;
-  if constexpr (sizeof(T) == 2) {
-    constexpr int C = Tl::BI / 8;   // units of a row
-    static_assert(Tl::BI * Tl::BJ * 2 <= Tl::LDS, "tile");
 #pragma unroll
-    for (int nj = 0; nj < Tl::NJ; ++nj) {
-      const int j = bj + 32 * nj + (lane & 31);
+  for (int nj = 0; nj < Tl::NJ; ++nj) {
+    const int j = bj + 32 * nj + (lane & 31);
 #pragma unroll
-      for (int mi = 0; mi < Tl::MI; ++mi)
+    for (int mi = 0; mi < Tl::MI; ++mi)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x2 lo = {acc[mi][nj][4 * q], acc[mi][nj][4 * q + 1]}, hi = {acc[mi][nj][4 * q + 2], acc[mi][nj][4 * q + 3]};
-          const int c = (bi + 32 * mi) / 8 + q;
-          *reinterpret_cast<u32x2*>(lds + j * (C * 16) + ((c ^ (j & (C - 1))) << 4) + (lane >> 5) * 8) =
-              (u32x2){__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)), __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
-        }
-    }
-    __syncthreads();
-    for (int u = threadIdx.x; u < Tl::BJ * C; u += Tl::NT) {
-      const int j = u / C, c = u % C;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(lds + j * (C * 16) + ((c ^ (j & (C - 1))) << 4));
-      if (j >= J) continue;
-      T* p = out + j * ldo + c * 8;
-      if (c * 8 + 8 <= I) {
-        store16(p, v);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (c * 8 + e < I) p[e] = T{(uint16_t)(v[e >> 1] >> (16 * (e & 1)))};
+      for (int q = 0; q < 4; ++q) {
+        const int i = bi + 32 * mi + entry_row(4 * q, lane);
+        const f32x4 v = {acc[mi][nj][4 * q], acc[mi][nj][4 * q + 1], acc[mi][nj][4 * q + 2], acc[mi][nj][4 * q + 3]};
+        if constexpr (sizeof(T) == 2) stage4<Tl>(lds, i, j, v[0], v[1], v[2], v[3]);
+        else if (j < J) write4(out + j * ldo + i, I - i, v);
+        if (sizeof(T) == 4) __builtin_amdgcn_sched_barrier(0);
       }
-    }
-  } else {
-#pragma unroll
-    for (int nj = 0; nj < Tl::NJ; ++nj) {
-      const int j = bj + 32 * nj + (lane & 31);
-      if (j >= J) continue;
-#pragma unroll
-      for (int mi = 0; mi < Tl::MI; ++mi)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int i = bi + 32 * mi + 8 * q + 4 * (lane >> 5);
-          T* p = out + j * ldo + i;
-          if (i + 4 <= I) {
-            store16(p, __builtin_bit_cast(u32x4, (f32x4){acc[mi][nj][4 * q], acc[mi][nj][4 * q + 1], acc[mi][nj][4 * q + 2], acc[mi][nj][4 * q + 3]}));
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (i + e < I) p[e] = acc[mi][nj][4 * q + e];
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        }
-    }
+  }
+  if constexpr (sizeof(T) == 2) {
+    __syncthreads();
+    write_staged<Tl>(lds, out, ldo, I, J);
   }
 }
 
@@ -601,13 +610,22 @@ __device__ __forceinline__ void add_tile(typename Tl::Acc& acc, const float* sum
   }
 }
 
-// sum over the 32 lanes of a half wavefront, in every lane of it
-__device__ __forceinline__ float sum32(float v) {
-  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x121, 0xf, 0xf, false));   // rotate 16 lanes by 1
-  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x122, 0xf, 0xf, false));   // by 2
-  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x124, 0xf, 0xf, false));   // by 4
-  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, false));   // by 8
-  return v + __shfl_xor(v, 16);
+// v plus what the lane `CTRL` (a rotation inside 16 lanes) says holds
+template <int CTRL>
+__device__ __forceinline__ float add_rotated(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
+}
+
+// Sums of a and b over the 32 lanes of a half wavefront: a's in its lanes 0 to
+// 15, b's in 16 to 31.
+__device__ __forceinline__ float sums32(float a, float b) {
+  // rows of 16 lanes 1 and 3 of the first change places with 0 and 2 of the second
+  const auto s = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), false, false);
+  float v = __builtin_bit_cast(float, (uint32_t)s[0]) + __builtin_bit_cast(float, (uint32_t)s[1]);
+  v = add_rotated<0x121>(v);
+  v = add_rotated<0x122>(v);
+  v = add_rotated<0x124>(v);
+  return add_rotated<0x128>(v);
 }
 
 // A tile of G: outputs m0 + i, rows j.
@@ -622,7 +640,9 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_dz_kernel(XArgs a) {
   typename Tl::Acc acc;
   Tl::product(a.W, a.A, i0, j0, 0, a.D, lds_address(lds), acc);
   const int bi = (wave / WJ) * 32 * Tl::MI, bj = (wave % WJ) * 32 * Tl::NJ;
-  add_bias<Tl>(acc, a.bias, i0 + bi, a.M);
+  float b[Tl::MI][16], cols[Tl::MI][16];
+  load_bias<Tl>(b, a.bias, i0 + bi, a.M);
+  T* out = static_cast<T*>(a.dz) + j0 * a.ldz + it * BI;
 #pragma unroll
   for (int nj = 0; nj < Tl::NJ; ++nj) {
     const int64_t j = j0 + bj + 32 * nj + (lane & 31);
@@ -633,28 +653,37 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_dz_kernel(XArgs a) {
     const int t = live ? target_at(target, a.M, i0 + bi) : -1;
 #pragma unroll
     for (int mi = 0; mi < Tl::MI; ++mi) {
+      float v[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[mi][nj][r] = exp_of(acc[mi][nj][r] - l);
+      for (int r = 0; r < 16; ++r) v[r] = exp_of(acc[mi][nj][r] + b[mi][r] - l);
       if (__any(t >= 32 * mi && t < 32 * mi + 32)) {
+        asm volatile("");   // (a branch: seldom taken)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (t == 32 * mi + entry_row(r, lane)) acc[mi][nj][r] -= 1.0f;
+          if (t == 32 * mi + entry_row(r, lane)) v[r] -= 1.0f;
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[mi][nj][r] = live ? acc[mi][nj][r] * g : 0.0f;
+      for (int r = 0; r < 16; ++r) {
+        v[r] = live ? v[r] * g : 0.0f;   // (whatever a row without a gradient has for logits)
+        cols[mi][r] = nj == 0 ? v[r] : cols[mi][r] + v[r];
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int i = bi + 32 * mi + entry_row(4 * q, lane);
+        if constexpr (sizeof(T) == 2) stage4<Tl>(lds, i, (int)(j - j0), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        else if (j < a.N) write4(out + (j - j0) * a.ldz + i, a.ldz - it * BI - i, (f32x4){v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]});
+      }
+      __builtin_amdgcn_sched_barrier(0);   // (a block at a time: few registers)
     }
   }
   // sums over the tile's rows, for the bias gradient
-  float* red = reinterpret_cast<float*>(lds);   // [WJ][BI]
+  float* red = reinterpret_cast<float*>(lds + (sizeof(T) == 2 ? Tl::BI * Tl::BJ * 2 : 0));   // [WJ][BI]
 #pragma unroll
   for (int mi = 0; mi < Tl::MI; ++mi)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      float s = acc[mi][0][r];
-#pragma unroll
-      for (int nj = 1; nj < Tl::NJ; ++nj) s += acc[mi][nj][r];
-      s = sum32(s);
-      if ((lane & 31) == 0) red[(wave % WJ) * BI + bi + 32 * mi + entry_row(r, lane)] = s;
+    for (int r = 0; r < 16; r += 2) {
+      const float s = sums32(cols[mi][r], cols[mi][r + 1]);
+      if ((lane & 15) == 0) red[(wave % WJ) * BI + bi + 32 * mi + entry_row(r, lane) + ((lane >> 4) & 1)] = s;
     }
   __syncthreads();
   for (int i = threadIdx.x; i < BI; i += Tl::NT) {
@@ -663,8 +692,7 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_dz_kernel(XArgs a) {
     for (int w = 1; w < WJ; ++w) s += red[w * BI + i];
     if (it * BI + i < a.ldz) a.cpart[jt * a.ldz + it * BI + i] = s;
   }
-  __syncthreads();
-  write_tile<T, Tl>(acc, lds, static_cast<T*>(a.dz) + j0 * a.ldz + it * BI, a.ldz, a.ldz - it * BI, a.N - j0);
+  if constexpr (sizeof(T) == 2) write_staged<Tl>(lds, out, a.ldz, a.ldz - it * BI, a.N - j0);
 }
 
 __global__ void __launch_bounds__(256) xent_dbias_kernel(const float* cpart, int64_t jtiles, int64_t ldz, int64_t n, float* out) {
@@ -747,11 +775,15 @@ hipError_t launch(K kernel, int lds, int64_t blocks, int splits, int threads, co
   return hipGetLastError();
 }
 
+// LDS of the kernel that forms G: the product's, or the staged tile and the sums behind it
+template <class T, class Tl>
+constexpr int kDzLds = sizeof(T) == 2 && Tl::BI * Tl::BJ * 2 + Tl::WJ * Tl::BI * 4 > (int)Tl::LDS ? Tl::BI * Tl::BJ * 2 + Tl::WJ * Tl::BI * 4 : (int)Tl::LDS;
+
 template <class T, bool GRAD, class Tl>
 hipError_t launch_logits(XArgs& a, int64_t outputs, hipStream_t s) {
   a.itiles = cdiv(outputs, Tl::BI);
   a.jtiles = cdiv(a.N, Tl::BJ);
-  if constexpr (GRAD) return launch(xent_dz_kernel<T, Tl>, Tl::LDS, a.itiles * a.jtiles, 1, Tl::NT, a, s);
+  if constexpr (GRAD) return launch(xent_dz_kernel<T, Tl>, kDzLds<T, Tl>, a.itiles * a.jtiles, 1, Tl::NT, a, s);
   else return launch(xent_tile_kernel<T, Tl>, Tl::LDS, a.itiles * a.jtiles, 1, Tl::NT, a, s);
 }
 
