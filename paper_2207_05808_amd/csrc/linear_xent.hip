@@ -185,21 +185,22 @@ struct Tile {
 
 // The tile of large bf16 products: 256 x 256 results of four wavefronts, 128 x
 // 128 each, one to a SIMD with its sums in the accumulation registers.  LDS
-// reads are then half of what the matrix cores take the time for (64 KB of
-// reads and 32 KB of writes per 32 k against 1024 cycles of 128 bytes), where
-// eight wavefronts of 128 x 64 would need all of it.  Steps of 32 k go from
-// memory straight to LDS through four buffers, three steps ahead.  A step's only
-// barrier stands between its two halves, when the second half's operands are in
-// registers; reads and transfers are issued between products, a few at a time,
-// since a wavefront waits where the memory pipeline's queue is full.
-// STAGED_X / STAGED_Y: an operand whose rows are not whole 16-byte units goes
-// through registers instead.
-template <Order OX, Order OY, bool STAGED_X, bool STAGED_Y>
+// reads are then half of what the matrix cores take the time for (128 KB of
+// reads and 64 KB of writes per 64 k against 2048 cycles of 128 bytes), where
+// eight wavefronts of 128 x 64 would need all of it.  Steps of 64 k (whole
+// 128-byte lines of rows along k) go from memory straight to LDS: five 32 KB
+// slots hold this step's two operands, the next step's and the first of the one
+// after.  A step's only barrier stands before its last quarter, whose operands
+// are in registers by then; the two slots that it frees are filled in the three
+// quarters that follow.  Reads and transfers are issued between products, a few
+// at a time, since a wavefront waits where the memory pipeline's queue is full.
+// STAGED_X: an operand X whose rows are not whole 16-byte units goes through
+// registers instead.
+template <Order OX, Order OY, bool STAGED_X>
 struct BigTile {
-  static constexpr int BI = 256, BJ = 256, BK = 32, WI = 2, WJ = 2, MI = 4, NJ = 4, NT = 256;
-  static constexpr int BUFFERS = 4;
-  static constexpr uint32_t OPB = 256 * BK * 2, STAGE = 2 * OPB, LDS = BUFFERS * STAGE;   // bytes of an operand's step, of a step, of all
-  static constexpr int U = 4;                                     // 16-byte units per thread, operand and step
+  static constexpr int BI = 256, BJ = 256, BK = 64, WI = 2, WJ = 2, MI = 4, NJ = 4, NT = 256;
+  static constexpr uint32_t SLOT = 256 * BK * 2, LDS = 5 * SLOT;
+  static constexpr int U = 8;                                     // 16-byte units per thread and operand of a step
   typedef f32x16 Acc[MI][NJ];
   typedef Tile<Bf16, OX, OY, 256, 256, 2, 2, BK> Small;           // the LDS layout and guarded loads are its
 
@@ -211,8 +212,8 @@ struct BigTile {
   static __device__ __forceinline__ uint32_t offset(const Operand& o, int64_t r0, int q) {
     const int lane = threadIdx.x & 63, block = (threadIdx.x >> 6) * U + q;
     if constexpr (O == kAlongK) {
-      int64_t r = block * 16 + (lane >> 2);
-      const int k = ((lane & 3) ^ ((r >> 2) & 3)) * 8;
+      int64_t r = block * 8 + (lane >> 3);
+      const int k = ((lane & 7) ^ ((r >> 1) & 7)) * 8;
       if (r > o.rows - 1 - r0) r = o.rows - 1 - r0;
       return (uint32_t)((r * o.ld + k) * 2);
     } else {
@@ -228,24 +229,21 @@ struct BigTile {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
   }
 
-  template <Order O, bool STAGED, int B>
+  template <Order O>
   struct Stream {
     const char* base;       // the next step's origin
     int64_t step;           // bytes from a step to the next
-    uint32_t to;            // this wavefront's part of a buffer
-    uint32_t off[STAGED ? 1 : U];
-    u32x4 held[STAGED ? U : 1];
+    uint32_t to;            // this wavefront's part of a slot
+    uint32_t off[U];
 
     __device__ __forceinline__ void init(const Operand& o, int64_t r0, int64_t k0, uint32_t lds) {
       base = static_cast<const char*>(o.p) + (O == kAlongK ? r0 * o.ld + k0 : k0 * o.ld + r0) * 2;
       step = (O == kAlongK ? (int64_t)BK : BK * o.ld) * 2;
       to = __builtin_amdgcn_readfirstlane(lds + (threadIdx.x >> 6) * (U * 1024));
-      if constexpr (!STAGED) {
 #pragma unroll
-        for (int q = 0; q < U; ++q) off[q] = offset<O>(o, r0, q);
-      }
+      for (int q = 0; q < U; ++q) off[q] = offset<O>(o, r0, q);
     }
-    // transfer q of the next step, into the buffer at `at`; the last one moves on
+    // transfer q of the next step, into the slot at `at`; the last one moves on
     __device__ __forceinline__ void send(int q, uint32_t at) {
       transfer(base, off[q], to + at + q * 1024);
       if (q == U - 1) base += step;
@@ -263,82 +261,86 @@ struct BigTile {
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[mi][nj][r] = 0.0f;
     const int steps = k0 < kend ? (int)((kend - k0) / BK) : 0;   // whole steps
-    Stream<OX, STAGED_X, 256> sx;
-    Stream<OY, STAGED_Y, 256> sy;
-    sx.init(X, i0, k0, lds);
-    sy.init(Y, j0, k0, lds + OPB);
-    auto send = [&](int s, int n) {   // transfer n = 0..7 of step s
-      const uint32_t at = (uint32_t)(s % BUFFERS) * STAGE;
-      if (n < U) {
-        if constexpr (!STAGED_X) sx.send(n, at);
-      } else {
-        if constexpr (!STAGED_Y) sy.send(n - U, at);
-      }
+    Stream<OX> sx;
+    Stream<OY> sy;
+    u32x4 held[STAGED_X ? U : 1];
+    if constexpr (!STAGED_X) sx.init(X, i0, k0, lds);
+    sy.init(Y, j0, k0, lds);
+    auto fetch = [&](int s) {   // a staged step to registers
+      if constexpr (STAGED_X) Small::template load<OX, 256, U>(X, i0, k0 + (int64_t)s * BK, kend, held);
     };
-    auto fetch = [&](int s) {
-      if constexpr (STAGED_X) Small::template load<OX, 256, U>(X, i0, k0 + (int64_t)s * BK, kend, sx.held);
-      if constexpr (STAGED_Y) Small::template load<OY, 256, U>(Y, j0, k0 + (int64_t)s * BK, kend, sy.held);
-    };
-    auto put = [&](int s) {
-      const uint32_t b = lds + (uint32_t)(s % BUFFERS) * STAGE;
-      if constexpr (STAGED_X) Small::template store<OX, 256, U>(b, sx.held);
-      if constexpr (STAGED_Y) Small::template store<OY, 256, U>(b + OPB, sy.held);
+    auto put = [&](uint32_t at) {   // and from there to its slot
+      if constexpr (STAGED_X) Small::template store<OX, 256, U>(lds + at, held);
     };
     bf16x8 x[2][MI], y[2][NJ];
-    auto read = [&](uint32_t b, int ks, int to, int n) {   // operand n = 0..7, in the order the products need them
-      if (n == 0 || n > NJ) x[to][n == 0 ? 0 : n - NJ] = Small::template frag<OX, 256>(b, bi + 32 * (n == 0 ? 0 : n - NJ), ks, lane);
-      else y[to][n - 1] = Small::template frag<OY, 256>(b + OPB, bj + 32 * (n - 1), ks, lane);
+    auto read = [&](uint32_t xs, uint32_t ys, int ks, int to, int n) {   // operand n = 0..7, in the order the products need them
+      if (n == 0 || n > NJ) x[to][n == 0 ? 0 : n - NJ] = Small::template frag<OX, 256>(lds + xs, bi + 32 * (n == 0 ? 0 : n - NJ), ks, lane);
+      else y[to][n - 1] = Small::template frag<OY, 256>(lds + ys, bj + 32 * (n - 1), ks, lane);
     };
-    // the 16 products of one half step, the next half's reads behind the first
-    // 8 of them and 4 transfers behind the others
-    auto half = [&](int from, uint32_t b, int ks, int s, int first, bool more) {
+    // the 16 products of one quarter step (16 k), the next quarter's reads
+    // behind the first 8 of them and 4 transfers, send(0..3), behind the others
+    auto quarter = [&](int from, uint32_t xs, uint32_t ys, int ks, auto send) {
 #pragma unroll
       for (int n = 0; n < MI * NJ; ++n) {
-        if (n < 8) read(b, ks, from ^ 1, n);
-        else if (more && (n & 1) == 0) send(s, first + (n - 8) / 2);
+        if (n < 8) read(xs, ys, ks, from ^ 1, n);
+        else if ((n & 1) == 0) send((n - 8) / 2);
         __builtin_amdgcn_sched_barrier(0);
         acc[n / NJ][n % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[from][n / NJ], y[from][n % NJ], acc[n / NJ][n % NJ], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    constexpr bool kStaged = STAGED_X || STAGED_Y;
     if (steps > 0) {
+      // slots in turn: X0 Y0 X1 Y1 X2, then Y2 where X0 was, X3 where Y0 was, ...
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+      for (int s = 0; s < 3; ++s)
         if (s < steps) {
-          if constexpr (kStaged) {
+          if constexpr (STAGED_X) {
             fetch(s);
-            put(s);
-          }
+            put(2 * s * SLOT);
+          } else {
 #pragma unroll
-          for (int n = 0; n < (s < 3 ? 8 : 4); ++n) send(s, n);
+            for (int q = 0; q < U; ++q) sx.send(q, 2 * s * SLOT);
+          }
+          if (s < 2) {
+#pragma unroll
+            for (int q = 0; q < U; ++q) sy.send(q, (2 * s + 1) * SLOT);
+          }
         }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (!STAGED_X && steps > 2) asm volatile("s_waitcnt vmcnt(24)" ::: "memory");   // step 0 is there
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (STAGED_X && steps > 3) fetch(3);
       lds_only_barrier();
 #pragma unroll
-      for (int n = 0; n < 8; ++n) read(lds, 0, 0, n);
-      // ALL: this step has four more behind it, so that every transfer is there to make
+      for (int n = 0; n < 8; ++n) read(0, SLOT, 0, 0, n);
+      auto next = [](uint32_t at) { return at + 2 * SLOT >= LDS ? at + 2 * SLOT - LDS : at + 2 * SLOT; };
+      uint32_t xs = 0, ys = SLOT, xb = 0, yb = 0;   // this step's slots, and the step's before
+      // ALL: a step that has one before it and three behind it
       auto step = [&](int s, auto all) {
         constexpr bool ALL = decltype(all)::value;
-        const uint32_t b = lds + (uint32_t)(s % BUFFERS) * STAGE;
-        if constexpr (kStaged) {
-          if (ALL || s + 4 < steps) fetch(s + 4);
+        const bool more_y = ALL || (s > 0 && s + 1 < steps), more_x = ALL || (s > 0 && s + 2 < steps), first_y = ALL || s + 2 < steps;
+        if constexpr (STAGED_X) {
+          if (more_x) {
+            put(yb);
+            if (ALL || s + 3 < steps) fetch(s + 3);
+          }
         }
-        half(0, b, 1, s + 3, 4, ALL || s + 3 < steps);
-        // every read of this buffer has arrived, and the next step's transfers
-        // have landed: at most those of the two steps after it are on their way
-        if constexpr (ALL && !kStaged) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
-        else if constexpr (ALL) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        quarter(0, xs, ys, 1, [&](int q) { if (more_y) sy.send(4 + q, xb); });
+        quarter(1, xs, ys, 2, [&](int q) { if (!STAGED_X && more_x) sx.send(q, yb); });
+        quarter(0, xs, ys, 3, [&](int q) { if (!STAGED_X && more_x) sx.send(4 + q, yb); });
+        // every read of this step has arrived, and the next step's transfers
+        // have landed: at most X of the step after it is on its way
+        if constexpr (ALL && !STAGED_X) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_only_barrier();
-        if constexpr (kStaged) {
-          if (ALL || s + 4 < steps) put(s + 4);
-        }
-        // (past the last step: reads of what is there, unused)
-        half(1, lds + (uint32_t)((s + 1) % BUFFERS) * STAGE, 0, s + 4, 0, ALL || s + 4 < steps);
+        xb = xs;
+        yb = ys;
+        xs = next(xs);
+        ys = next(ys);
+        quarter(1, xs, ys, 0, [&](int q) { if (first_y) sy.send(q, xb); });   // (past the last step: reads of what is there, unused)
       };
-      int s = 0;
-      for (; s + 4 < steps; ++s) step(s, std::true_type{});
+      step(0, std::false_type{});
+      int s = 1;
+      for (; s + 3 < steps; ++s) step(s, std::true_type{});
       for (; s < steps; ++s) step(s, std::false_type{});
       __syncthreads();
     }
@@ -347,11 +349,11 @@ struct BigTile {
       Small::template load<OX, 256, U>(X, i0, k0 + (int64_t)steps * BK, kend, v);
       Small::template store<OX, 256, U>(lds, v);
       Small::template load<OY, 256, U>(Y, j0, k0 + (int64_t)steps * BK, kend, v);
-      Small::template store<OY, 256, U>(lds + OPB, v);
+      Small::template store<OY, 256, U>(lds + SLOT, v);
       __syncthreads();
-      for (int ks = 0; ks < 2; ++ks) {
+      for (int ks = 0; ks < 4; ++ks) {
 #pragma unroll
-        for (int n = 0; n < 8; ++n) read(lds, ks, 0, n);
+        for (int n = 0; n < 8; ++n) read(0, SLOT, ks, 0, n);
 #pragma unroll
         for (int n = 0; n < MI * NJ; ++n)
           acc[n / NJ][n % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[0][n / NJ], y[0][n % NJ], acc[n / NJ][n % NJ], 0, 0, 0);
@@ -698,7 +700,15 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_dz_kernel(XArgs a) {
 __global__ void __launch_bounds__(256) xent_dbias_kernel(const float* cpart, int64_t jtiles, int64_t ldz, int64_t n, float* out) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     float s = 0.0f;
-    for (int64_t j = 0; j < jtiles; ++j) s += cpart[j * ldz + i];
+    int64_t j = 0;
+    for (; j + 8 <= jtiles; j += 8) {   // eight loads under way at a time
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = cpart[(j + k) * ldz + i];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += v[k];
+    }
+    for (; j < jtiles; ++j) s += cpart[j * ldz + i];
     out[i] = s;
   }
 }
@@ -806,10 +816,10 @@ template <class T, bool GRAD>
 hipError_t logits(XArgs& a, int64_t outputs, int rows, bool md, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
     if (rows == 256) {
-      if (direct(a.W, !md)) return md ? launch_logits<T, GRAD, BigTile<kAlongK, kAlongK, false, false>>(a, outputs, s)
-                                 : launch_logits<T, GRAD, BigTile<kAlongI, kAlongK, false, false>>(a, outputs, s);
-      return md ? launch_logits<T, GRAD, BigTile<kAlongK, kAlongK, true, false>>(a, outputs, s)
-                : launch_logits<T, GRAD, BigTile<kAlongI, kAlongK, true, false>>(a, outputs, s);
+      if (direct(a.W, !md)) return md ? launch_logits<T, GRAD, BigTile<kAlongK, kAlongK, false>>(a, outputs, s)
+                                 : launch_logits<T, GRAD, BigTile<kAlongI, kAlongK, false>>(a, outputs, s);
+      return md ? launch_logits<T, GRAD, BigTile<kAlongK, kAlongK, true>>(a, outputs, s)
+                : launch_logits<T, GRAD, BigTile<kAlongI, kAlongK, true>>(a, outputs, s);
     }
   }
   if (rows >= 128) return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>>(a, outputs, s)
@@ -867,8 +877,8 @@ GradPlan grad_plan(int64_t N, int64_t D, int64_t M, int64_t elem) {
   g.off_dz = take(N * g.p * elem);
   g.off_c = take(cdiv(N, 32) * g.p * 4);
   g.off_sum = take(g.p < M ? N * D * 4 : 0);
-  // shares of a product: at most kSlots tiles of 128 x 128
-  g.part = (int64_t)kSlots * 128 * 128 * 4;
+  // shares of a product: a tile of 256 x 256 for each compute unit
+  g.part = 256ll * 256 * 256 * 4;
   g.off_part = take(g.part);
   g.total = off;
   return g;
@@ -904,8 +914,8 @@ hipError_t grad(XArgs a, bool md, void* dA, void* dB, float* dbias, char* ws, hi
     if constexpr (sizeof(T) == 2) {
       if (a.N >= 256 && a.D >= 256) {
         done = true;
-        if (direct(x.X, md)) e = md ? gemm<T, BigTile<kAlongI, kAlongK, false, false>, true>(x, g.part, s) : gemm<T, BigTile<kAlongK, kAlongK, false, false>, true>(x, g.part, s);
-        else e = md ? gemm<T, BigTile<kAlongI, kAlongK, true, false>, true>(x, g.part, s) : gemm<T, BigTile<kAlongK, kAlongK, true, false>, true>(x, g.part, s);
+        if (direct(x.X, md)) e = md ? gemm<T, BigTile<kAlongI, kAlongK, false>, true>(x, g.part, s) : gemm<T, BigTile<kAlongK, kAlongK, false>, true>(x, g.part, s);
+        else e = md ? gemm<T, BigTile<kAlongI, kAlongK, true>, true>(x, g.part, s) : gemm<T, BigTile<kAlongK, kAlongK, true>, true>(x, g.part, s);
       }
     }
     if (done) {}
@@ -923,7 +933,7 @@ hipError_t grad(XArgs a, bool md, void* dA, void* dB, float* dbias, char* ws, hi
     if constexpr (sizeof(T) == 2) {
       if (direct(ai, true) && cdiv(a.D, 256) * cdiv(n, 256) >= 192) {
         done = true;
-        e = gemm<T, BigTile<kAlongI, kAlongI, false, false>, false>(x, g.part, s);
+        e = gemm<T, BigTile<kAlongI, kAlongI, false>, false>(x, g.part, s);
       }
     }
     if (!done) e = gemm<T, Tile<T, kAlongI, kAlongI, 128, 128, 2, 2>, false>(x, g.part, s);
