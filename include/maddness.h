@@ -442,15 +442,25 @@ int maddness_dequantize_w4(const uint8_t* codes, const uint8_t* exps, int32_t D,
  * maddness_matmul_act (a bias is not used with MADDNESS_ACT_NONE).
  *   A      [N][lda], dtype fp32, bf16 or fp16; any alignment of its rows.
  *   y_out  [N][M] dense, y_dtype fp32 or A's; a row softmax needs fp32.
- * Products are exact (fp32 activations as three bf16 parts, fp16 as two) and
- * summed in 32 bits, in an order that the shape fixes; y is rounded once.
+ * Products are exact (fp32 activations as three bf16 parts) and summed in 32
+ * bits, in an order that the shape fixes; y is rounded once.  (fp16 activations
+ * and many rows: a column's groups more than 35 octaves below its largest lose
+ * bits, 2^-36 of that one and less.)
+ * workspace: for many rows the weights are unpacked first, a piece at a time,
+ * into maddness_matmul_w4_workspace_bytes(...) device bytes, 256-byte aligned,
+ * contents undefined on return; 0 where a call uses none.  NULL: the call runs
+ * without, slower.  The size depends on A's alignment: pass the A of the call.
  * EINVAL: act or a dtype out of range, lda < D, a NULL array (when N > 0),
- * codes not 16-byte or exps not 4-byte aligned.  N == 0 enqueues nothing.
+ * codes not 16-byte or exps not 4-byte aligned, a workspace that is too small.
+ * N == 0 enqueues nothing.
  */
+int64_t maddness_matmul_w4_workspace_bytes(const void* A, int32_t dtype, int64_t N,
+                                           int32_t D, int64_t lda, int32_t M);   /* -1 if out of range */
 int maddness_matmul_w4(const void* A, int32_t dtype, int64_t N, int32_t D,
                        int64_t lda, const uint8_t* codes, const uint8_t* exps,
                        int32_t M, const float* col_bias, int32_t act, void* y_out,
-                       int32_t y_dtype, void* stream);
+                       int32_t y_dtype, void* workspace, int64_t workspace_bytes,
+                       void* stream);
 
 /*
  * Softmax cross entropy of an output layer, without keeping its logits: with

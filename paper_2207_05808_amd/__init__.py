@@ -14,7 +14,7 @@ _BINDING = ("encode", "lut_accumulate", "lut_accumulate_f32", "matmul", "matmul_
             "build_lut", "build_lut_f32", "quantize_lut", "encoder_gram", "encoder_scatter", "fit_lut_ridge", "fit_lut_gd",
             "fit_lut_workspace_bytes", "fit_lut_gd_workspace_bytes", "matmul_index_bytes", "matmul_noalloc",
             "version", "prepare_matmul", "prepare_matmul_f32", "PreparedCall", "W4Weights", "quantize_w4", "dequantize_w4",
-            "matmul_w4", "linear_xent", "linear_xent_grad", "linear_xent_workspace_bytes", "linear_xent_grad_workspace_bytes")
+            "matmul_w4", "matmul_w4_workspace_bytes", "linear_xent", "linear_xent_grad", "linear_xent_workspace_bytes", "linear_xent_grad_workspace_bytes")
 
 __all__ = list(_BINDING) + ["MaddnessError"]
 

@@ -79,7 +79,9 @@ def lib() -> ctypes.CDLL:
         L.maddness_w4_exponent_bytes.restype = i64
         L.maddness_quantize_w4.argtypes = [vp, i32, i32, i32, i64, i64, vp, vp, vp]
         L.maddness_dequantize_w4.argtypes = [vp, vp, i32, i32, vp, i32, vp]
-        L.maddness_matmul_w4.argtypes = [vp, i32, i64, i32, i64, vp, vp, i32, vp, i32, vp, i32, vp]
+        L.maddness_matmul_w4_workspace_bytes.argtypes = [vp, i32, i64, i32, i64, i32]
+        L.maddness_matmul_w4_workspace_bytes.restype = i64
+        L.maddness_matmul_w4.argtypes = [vp, i32, i64, i32, i64, vp, vp, i32, vp, i32, vp, i32, vp, i64, vp]
         for f in ("maddness_linear_xent_workspace_bytes", "maddness_linear_xent_grad_workspace_bytes"):
             getattr(L, f).argtypes = [i64, i32, i32, i32]
             getattr(L, f).restype = i64

@@ -804,12 +804,15 @@ def dequantize_w4(w: W4Weights, dtype=torch.bfloat16, out=None, stream=None):
     return out
 
 
-def matmul_w4(A, w: W4Weights, col_bias=None, act=None, out_dtype=None, y_out=None, stream=None):
+def matmul_w4(A, w: W4Weights, col_bias=None, act=None, out_dtype=None, y_out=None, workspace=None, stream=None):
     """Layer with 4-bit weights, sigma(A W + col_bias); returns y [N, M].
 
     A [N, D] fp32, bf16 or fp16 with dense columns.  act "none" (no bias),
     "bias", "relu" or "softmax"; None: "bias" where one is given.  y has A's
-    dtype, or out_dtype torch.float32, which a softmax always gives."""
+    dtype, or out_dtype torch.float32, which a softmax always gives.
+    ``workspace``: an optional uint8 device tensor of at least
+    matmul_w4_workspace_bytes(A, M) bytes (+ up to 255 for alignment), used for
+    many rows; allocated when None."""
     code = _typed(A, "A", (torch.float32, torch.bfloat16, torch.float16), 2)
     D, M = _w4(w)
     N = A.shape[0]
@@ -827,10 +830,23 @@ def matmul_w4(A, w: W4Weights, col_bias=None, act=None, out_dtype=None, y_out=No
         raise TypeError("a softmax gives torch.float32")
     with _device(A.device):
         y_out = _output(y_out, "y_out", (N, M), out_dtype, A.device)
+        need, wp = int(_lib.lib().maddness_matmul_w4_workspace_bytes(_ptr(A), code, N, D, lda, M)), None
+        if need > 0:
+            workspace, wp = _scratch(workspace, need, A.device, stream)
         st = _lib.lib().maddness_matmul_w4(_ptr(A), code, N, D, lda, _ptr(w.codes), _ptr(w.exps), M, _ptr(col_bias), a,
-                                           _ptr(y_out), DTYPE[out_dtype], _stream(stream))
+                                           _ptr(y_out), DTYPE[out_dtype], wp, need, _stream(stream))
     _lib.check("maddness_matmul_w4", st)
     return y_out
+
+
+def matmul_w4_workspace_bytes(A, M: int) -> int:
+    """Device bytes of workspace that matmul_w4 uses for this A (its shape,
+    type and alignment) and M outputs; 0 where it uses none."""
+    code = _typed(A, "A", (torch.float32, torch.bfloat16, torch.float16), 2)
+    n = int(_lib.lib().maddness_matmul_w4_workspace_bytes(_ptr(A), code, A.shape[0], A.shape[1], _row_stride(A), M))
+    if n < 0:
+        _lib.check("maddness_matmul_w4_workspace_bytes", _lib.EINVAL)
+    return n
 
 
 def _xent_inputs(A, B, target, col_bias):

@@ -6,9 +6,7 @@
 // bits of mantissa times a power of two are exact in bf16, and one instruction
 // unpacks two codes and scales them, so a weight costs half an instruction and
 // the scale none after the product.
-#include "maddness.h"
-#include "internal.hpp"
-#include "mma.hpp"
+#include "tile.hpp"
 
 namespace mdn {
 namespace {
@@ -244,8 +242,136 @@ __global__ void __launch_bounds__(256) w4_dequantize_kernel(DArgs a) {
   }
 }
 
-bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-int status_from(hipError_t e) { return e == hipSuccess ? MADDNESS_OK : MADDNESS_EHIP; }
+// ------------------------------------------------------------ many rows
+// The weights are unpacked to 16 bits once, k contiguous, and go through the
+// tile product: bf16 (exact), or for fp16 activations fp16 with each column's
+// weights scaled so that its largest exponent becomes 2^12 (its groups stay
+// exact down to 35 octaves below that; the product is scaled back).  fp32
+// activations become three bf16 parts side by side, over which the weights'
+// k runs three times.
+
+struct EArgs {
+  const uint8_t* codes; const uint8_t* exps; int nk;
+  int64_t rows;        // columns of the weights in this piece (rows of the result)
+  void* W; int64_t ld; // [rows][ld], ld = 128 nk
+  int32_t* shift;      // [16 * blocks]: the power of two a column's results are to be scaled by (fp16)
+};
+
+// One workgroup per 16 columns.
+template <class T>
+__global__ void __launch_bounds__(256) w4_unpack_kernel(EArgs a) {
+  __shared__ int top[256];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
+  const int64_t mb = blockIdx.x;
+  const uint32_t* exps = reinterpret_cast<const uint32_t*>(a.exps) + mb * a.nk * 16;
+  int ref = 127;
+  if constexpr (std::is_same<T, F16>::value) {
+    int most = 0;   // largest exponent of the column, NaN groups (255) aside
+    for (int e = threadIdx.x; e < a.nk * 16; e += 256) {
+      const uint32_t w = exps[e];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int b = (int)((w >> (8 * j)) & 0xff);
+        if (b != 255 && b > most) most = b;
+      }
+    }
+    top[threadIdx.x] = most;
+    __syncthreads();
+    for (int t = 0; t < 16; ++t) most = top[t * 16 + col] > most ? top[t * 16 + col] : most;
+    ref = most - 12;
+    if (threadIdx.x < 16) a.shift[mb * 16 + threadIdx.x] = ref - 127;
+  }
+  const int64_t row = mb * 16 + col;
+  T* out = static_cast<T*>(a.W) + row * a.ld;
+  for (int kb = wave; kb < a.nk; kb += 4) {
+    const u32x4 w = (reinterpret_cast<const u32x4*>(a.codes) + (mb * a.nk + kb) * 64)[lane];
+    const uint32_t e = exps[kb * 16 + col];
+    if (row >= a.rows) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      u32x4 v;
+      if constexpr (std::is_same<T, F16>::value) {
+        const int b = (int)((e >> (8 * j)) & 0xff);
+        const float s = b == 255 ? __uint_as_float(0x7f800000u) : ldexpf(1.0f, b - ref < -60 ? -60 : b - ref);
+        v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[j], s, 0));
+        v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[j], s, 1));
+        v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[j], s, 2));
+        v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w[j], s, 3));
+      } else {
+        v = __builtin_bit_cast(u32x4, unpack8(w[j], scale_of(e, j)));
+      }
+      *reinterpret_cast<u32x4*>(out + kb * kWK + 32 * j + 8 * quarter) = v;
+    }
+  }
+}
+
+struct PArgs {
+  const void* A; int64_t N, lda; int D;
+  void* out; int64_t ld; int per;   // [N][parts * per], `per` columns a part, zeros behind the D there are
+};
+
+// Rows of A as 16-bit parts side by side, 8 columns a thread.
+template <class T>
+__global__ void __launch_bounds__(256) w4_parts_kernel(PArgs a) {
+  const int units = a.per / 8;
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < a.N * units; u += (int64_t)gridDim.x * 256) {
+    const int64_t n = u / units;
+    const int k = (int)(u % units) * 8;
+    const T* p = static_cast<const T*>(a.A) + n * a.lda + k;
+    uint16_t* out = static_cast<uint16_t*>(a.out) + n * a.ld + k;
+    if constexpr (sizeof(T) == 2) {
+      const Bf16* q = reinterpret_cast<const Bf16*>(p);   // (the bits as they are)
+      bf16x8 x[1];
+      load_parts<Bf16>(q, a.D - k, x);
+      *reinterpret_cast<u32x4*>(out) = __builtin_bit_cast(u32x4, x[0]);
+    } else {
+      bf16x8 x[Parts<T>::n];
+      load_parts<T>(p, a.D - k, x);
+#pragma unroll
+      for (int s = 0; s < Parts<T>::n; ++s) *reinterpret_cast<u32x4*>(out + s * a.per) = __builtin_bit_cast(u32x4, x[s]);
+    }
+  }
+}
+
+struct WTArgs {
+  Operand W, A;
+  int64_t K, N, M;             // M: outputs from this piece's first on
+  const float* bias;           // of this piece, or null
+  const int32_t* shift;        // of this piece (fp16)
+  int act;
+  void* y; int64_t ldy;
+  int64_t itiles, jtiles;
+};
+
+template <class T, class Y, class Tl>
+__global__ void __launch_bounds__(Tl::NT, 1) w4_tile_kernel(WTArgs a) {
+  extern __shared__ __align__(16) char lds[];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t it, jt;
+  tile_of(blockIdx.x, a.itiles, a.jtiles, it, jt);
+  const int64_t i0 = it * Tl::BI, j0 = jt * Tl::BJ;
+  typename Tl::Acc acc;
+  Tl::product(a.W, a.A, i0, j0, 0, a.K, lds_address(lds), acc);
+  const int bi = (wave / Tl::WJ) * 32 * Tl::MI;
+#pragma unroll
+  for (int mi = 0; mi < Tl::MI; ++mi)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int64_t i = i0 + bi + 32 * mi + entry_row(r, lane), at = i < a.M ? i : a.M - 1;
+      const float b = a.bias ? a.bias[at] : 0.0f;
+      const int e = std::is_same<T, F16>::value ? a.shift[at] : 0;
+#pragma unroll
+      for (int nj = 0; nj < Tl::NJ; ++nj) {
+        float v = acc[mi][nj][r];
+        if constexpr (std::is_same<T, F16>::value) v = ldexpf(v, e);
+        v += b;
+        acc[mi][nj][r] = a.act == 2 && !(v > 0.0f) ? 0.0f : v;
+      }
+      if ((r & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+  write_tile<Y, Tl>(acc, lds, static_cast<Y*>(a.y) + j0 * a.ldy + i0, a.ldy, a.M - i0, a.N - j0);
+}
+
 int blocks_for(int64_t waves, int per) {
   const int64_t b = (waves + per - 1) / per, most = 1 << 20;
   return (int)(b < most ? b : most);
@@ -260,8 +386,81 @@ hipError_t launch_rows(const WArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// From how many rows on the weights are unpacked first.
+constexpr int64_t kManyRows = 128;
+
+// The plan for many rows; bytes: workspace, 0 where the rows kernel takes the call.
+struct Many {
+  int parts; bool direct;   // 16-bit parts of A; A's rows go to LDS as they are
+  int64_t per, piece, off_shift, off_w, bytes;
+};
+Many plan_many(const void* A, int32_t dtype, int64_t N, int32_t D, int64_t lda, int32_t M) {
+  Many p{};
+  if (N <= kManyRows) return p;
+  p.parts = dtype == MADDNESS_F32 ? 3 : 1;
+  p.direct = dtype != MADDNESS_F32 && D % 64 == 0 && direct(Operand{A, lda, N, N, 0}, false);
+  p.per = ((int64_t)D + kWK - 1) / kWK * kWK;
+  // outputs at a time: their 16-bit weights within 256 MiB, at least 256 outputs
+  p.piece = (128ll << 20) / p.per / 256 * 256;
+  if (p.piece < 256) p.piece = 256;
+  if (p.piece > up(M, 16)) p.piece = up(M, 16);
+  int64_t off = p.direct ? 0 : up(N * p.parts * p.per * 2, 256);
+  p.off_shift = off;
+  off += dtype == MADDNESS_F16 ? up(p.piece * 4, 256) : 0;
+  p.off_w = off;
+  p.bytes = off + up(p.piece * p.per * 2, 256);
+  return p;
+}
+
+template <class T, class Y, class Tl>
+hipError_t launch_tile(WTArgs& a, hipStream_t s) {
+  a.itiles = cdiv(a.M, Tl::BI);
+  a.jtiles = cdiv(a.N, Tl::BJ);
+  return launch(w4_tile_kernel<T, Y, Tl>, Tl::LDS, a.itiles * a.jtiles, 1, Tl::NT, a, s);
+}
+
+// T: what the tiles multiply (bf16, or fp16 for fp16 activations)
+template <class A, class T, class Y>
+hipError_t launch_many(const WArgs& a, const Many& p, char* ws, hipStream_t s) {
+  WTArgs t{};
+  t.A = Operand{a.A, a.lda, a.N, a.N, 0};
+  t.K = a.D;
+  if (!p.direct) {
+    PArgs q{a.A, a.N, a.lda, a.D, ws, p.parts * p.per, (int)p.per};
+    hipLaunchKernelGGL((w4_parts_kernel<A>), dim3(blocks_for(a.N * (p.per / 8), 256)), dim3(256), 0, s, q);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    t.A = Operand{ws, p.parts * p.per, a.N, a.N, 0};
+    t.K = p.parts * p.per;
+  }
+  t.N = a.N; t.act = a.act; t.ldy = a.M;
+  t.shift = reinterpret_cast<int32_t*>(ws + p.off_shift);
+  for (int64_t m0 = 0; m0 < a.M; m0 += p.piece) {
+    const int64_t n = a.M - m0 < p.piece ? a.M - m0 : p.piece, at = m0 / kWM * a.nk;
+    EArgs e{a.codes + at * 1024, a.exps + at * 64, a.nk, n, ws + p.off_w, p.per, reinterpret_cast<int32_t*>(ws + p.off_shift)};
+    hipLaunchKernelGGL((w4_unpack_kernel<T>), dim3((unsigned)cdiv(n, kWM)), dim3(256), 0, s, e);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    t.W = Operand{ws + p.off_w, p.per, n, n, p.per};
+    t.M = n;
+    t.bias = a.bias ? a.bias + m0 : nullptr;
+    t.y = static_cast<Y*>(a.y) + m0;
+    // 256 x 256 tiles where they leave work for most compute units
+    if (p.direct || p.parts * p.per <= (1 << 22)) {
+      if (a.N >= 192 && cdiv(a.N, 256) * cdiv(n, 256) >= 192) err = launch_tile<T, Y, BigTile<T, kAlongK, kAlongK, false>>(t, s);
+      else err = launch_tile<T, Y, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>>(t, s);
+    } else {
+      err = launch_tile<T, Y, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>>(t, s);
+    }
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
+}
+
 template <class T, class Y>
-hipError_t launch_w4(const WArgs& a, hipStream_t stream) {
+hipError_t launch_w4(const WArgs& a, const Many& p, char* ws, hipStream_t stream) {
+  if (p.bytes > 0 && ws)
+    return launch_many<T, typename std::conditional<std::is_same<T, F16>::value, F16, Bf16>::type, Y>(a, p, ws, stream);
   if (a.N <= 16) return launch_rows<T, Y, 1>(a, stream);
   if (a.N <= 32) return launch_rows<T, Y, 2>(a, stream);
   return launch_rows<T, Y, 4>(a, stream);
@@ -311,9 +510,14 @@ int maddness_dequantize_w4(const uint8_t* codes, const uint8_t* exps, int32_t D,
   return status_from(hipGetLastError());
 }
 
+int64_t maddness_matmul_w4_workspace_bytes(const void* A, int32_t dtype, int64_t N, int32_t D, int64_t lda, int32_t M) {
+  if (N < 0 || D <= 0 || M <= 0 || lda < D || dtype < MADDNESS_F32 || dtype > MADDNESS_F16) return -1;
+  return plan_many(A, dtype, N, D, lda, M).bytes;
+}
+
 int maddness_matmul_w4(const void* A, int32_t dtype, int64_t N, int32_t D, int64_t lda, const uint8_t* codes,
                        const uint8_t* exps, int32_t M, const float* col_bias, int32_t act, void* y_out,
-                       int32_t y_dtype, void* stream) {
+                       int32_t y_dtype, void* workspace, int64_t workspace_bytes, void* stream) {
   if (N < 0 || D <= 0 || M <= 0 || lda < D || act < 0 || act > 3) return MADDNESS_EINVAL;
   if (dtype < MADDNESS_F32 || dtype > MADDNESS_F16 || (y_dtype != dtype && y_dtype != MADDNESS_F32)) return MADDNESS_EINVAL;
   if (act == MADDNESS_ACT_SOFTMAX && y_dtype != MADDNESS_F32) return MADDNESS_EINVAL;
@@ -322,13 +526,16 @@ int maddness_matmul_w4(const void* A, int32_t dtype, int64_t N, int32_t D, int64
   if (!aligned(A, dtype == MADDNESS_F32 ? 4 : 2) || !aligned(y_out, y_dtype == MADDNESS_F32 ? 4 : 2) || !aligned(codes, 16) ||
       !aligned(exps, 4) || (col_bias && !aligned(col_bias, 4)))
     return MADDNESS_EINVAL;
+  const Many p = plan_many(A, dtype, N, D, lda, M);
+  if (workspace && p.bytes > 0 && (!aligned(workspace, 256) || workspace_bytes < p.bytes)) return MADDNESS_EINVAL;
+  char* ws = static_cast<char*>(workspace);
   WArgs a{A, N, lda, D, M, codes, exps, act == MADDNESS_ACT_NONE ? nullptr : col_bias, act == MADDNESS_ACT_RELU ? 2 : 0, y_out,
           (int)(((int64_t)D + kWK - 1) / kWK), (int)(((int64_t)M + kWM - 1) / kWM)};
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;
-  if (dtype == MADDNESS_F32) e = launch_w4<float, float>(a, s);
-  else if (dtype == MADDNESS_BF16) e = y_dtype == MADDNESS_F32 ? launch_w4<Bf16, float>(a, s) : launch_w4<Bf16, Bf16>(a, s);
-  else e = y_dtype == MADDNESS_F32 ? launch_w4<F16, float>(a, s) : launch_w4<F16, F16>(a, s);
+  if (dtype == MADDNESS_F32) e = launch_w4<float, float>(a, p, ws, s);
+  else if (dtype == MADDNESS_BF16) e = y_dtype == MADDNESS_F32 ? launch_w4<Bf16, float>(a, p, ws, s) : launch_w4<Bf16, Bf16>(a, p, ws, s);
+  else e = y_dtype == MADDNESS_F32 ? launch_w4<F16, float>(a, p, ws, s) : launch_w4<F16, F16>(a, p, ws, s);
   if (e != hipSuccess || act != MADDNESS_ACT_SOFTMAX) return status_from(e);
   hipLaunchKernelGGL(w4_softmax_kernel, dim3((unsigned)(N < 65535 ? N : 65535)), dim3(1024), 0, s, static_cast<float*>(y_out), N, M);
   return status_from(hipGetLastError());

@@ -141,6 +141,45 @@ def test_matmul(N, D, M, dtype):
     check(rand((N, D), 4, dtype), w, None, "none")
 
 
+@pytest.mark.parametrize("N,D,M", [(2500, 128, 5000), (3000, 321, 4099), (257, 64, 50003)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_many_rows(N, D, M, dtype):
+    """More tiles than compute units; with the caller's workspace (dirty) and
+    with none at all, which takes the kernel of few rows."""
+    w = mdn.quantize_w4(rand((D, M), 3) * D ** -0.5)
+    A, bias = rand((N, D), 4, dtype), rand((M,), 5)
+    y = check(A, w, bias, "relu")
+    ws = torch.full((mdn.matmul_w4_workspace_bytes(A, M) + 255,), 255, dtype=torch.uint8, device=DEV)
+    assert torch.equal(mdn.matmul_w4(A, w, col_bias=bias, act="relu", workspace=ws), y)
+    with pytest.raises(ValueError):
+        mdn.matmul_w4(A, w, workspace=ws[:1000])
+    z = mdn.matmul_w4(A, w, col_bias=bias, act="relu", out_dtype=torch.float32)
+    few = torch.cat([mdn.matmul_w4(A[n:n + 64], w, col_bias=bias, act="relu", out_dtype=torch.float32) for n in (0, 64, N - 64)])
+    many = torch.cat([z[:128], z[N - 64:]])
+    assert torch.allclose(many, few, rtol=1e-4, atol=1e-4)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_exponents_far_apart(dtype):
+    """Groups of one column 30 octaves apart, columns of the largest and the
+    smallest exponents: exact weights all the same."""
+    D, M = 128, 300
+    B = rand((D, M), 3)
+    B[32:64] *= 2.0 ** -30
+    B[:, 10] *= 2.0 ** 100
+    B[:, 11] *= 2.0 ** -80
+    B[:, 12] = 0.0
+    w = mdn.quantize_w4(B)
+    A = rand((300, D), 4, dtype)
+    A[:, :32] = 0
+    A[:, 64:] = 0     # only the small groups are left
+    W = mdn.dequantize_w4(w, dtype=torch.float32).double()
+    for rows in (A, A[:9]):
+        y = mdn.matmul_w4(rows, w, out_dtype=torch.float32).double()
+        ref, size = rows.double() @ W, rows.double().abs() @ W.abs()
+        assert bool(((y - ref).abs() <= size * 70 * 2.0 ** -23).all())
+
+
 @pytest.mark.parametrize("N,D,M", [(1, 256, 130), (5, 300, 7), (70, 129, 1003), (300, 512, 512)])
 @pytest.mark.parametrize("act", ["bias", "relu", "softmax"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -195,7 +234,7 @@ def test_values_that_are_not_finite(dtype):
     B[7, 9] = 0.0
     w = mdn.quantize_w4(B)
     W = mdn.dequantize_w4(w, dtype=torch.float32)
-    for N in (4, 90):
+    for N in (4, 90, 300):
         A = rand((N, D), 4, dtype)
         A[1, 7] = math.inf
         A[2, 100] = math.nan
@@ -208,8 +247,9 @@ def test_values_that_are_not_finite(dtype):
     half = mdn.quantize_w4(torch.full((D, 1), 2.0 ** -20, device=DEV))
     check(big, half, None, "none", torch.float32)
     B[150, 3] = math.nan
-    y = mdn.matmul_w4(rand((4, D), 4, dtype), mdn.quantize_w4(B))
-    assert y[:, 3].isnan().all() and torch.isfinite(y[:, 4:]).all()
+    for N in (4, 300):
+        y = mdn.matmul_w4(rand((N, D), 4, dtype), mdn.quantize_w4(B))
+        assert y[:, 3].isnan().all() and torch.isfinite(y[:, 4:]).all()
 
 
 def test_refusals():
