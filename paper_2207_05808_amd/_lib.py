@@ -120,7 +120,9 @@ def calls():
         L = lib()
         m.init(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in (
             "maddness_matmul", "maddness_matmul_f32", "maddness_matmul_act", "maddness_matmul_act_f32",
-            "maddness_matmul_index_bytes")))
+            "maddness_matmul_index_bytes", "maddness_matmul_w4", "maddness_matmul_w4_workspace_bytes",
+            "maddness_quantize_w4", "maddness_dequantize_w4", "maddness_linear_xent_workspace_bytes",
+            "maddness_linear_xent", "maddness_linear_xent_grad_workspace_bytes", "maddness_linear_xent_grad")))
         _calls = m
     return _calls or None
 

@@ -706,6 +706,26 @@ def _same_device(device, **tensors):
             raise ValueError(f"{name} must be on {device}, got {t.device}")
 
 
+def _plain_call(name, *args):
+    """One of the natively marshalled calls on the current device and stream;
+    None when the arguments are not its plain valid case (the caller then goes
+    through its own checks), or there is no native marshalling."""
+    global _calls
+    if _calls is None:
+        _calls = _lib.calls() or False
+    if not _calls:
+        return None
+    device = torch._C._cuda_getDevice()
+    return getattr(_calls, name)(*args, device, torch._C._cuda_getCurrentRawStream(device))
+
+
+_calls = None
+
+
+def _on_gpu(t) -> bool:
+    return type(t) is torch.Tensor and t.is_cuda
+
+
 @contextlib.contextmanager
 def _device(device):
     """The device of the call's tensors as the current one."""
@@ -778,6 +798,10 @@ def _w4(w):
 def quantize_w4(B, stream=None) -> W4Weights:
     """4-bit block floating point weights of B [D, M] (fp32, bf16 or fp16, any
     strides); see maddness_quantize_w4."""
+    if stream is None and _on_gpu(B):
+        r = _plain_call("quantize", B)
+        if r is not None:
+            return W4Weights(*r, *B.shape)
     code = _typed(B, "B", (torch.float32, torch.bfloat16, torch.float16), 2)
     D, M = B.shape
     if D == 0 or M == 0:
@@ -794,6 +818,10 @@ def quantize_w4(B, stream=None) -> W4Weights:
 
 def dequantize_w4(w: W4Weights, dtype=torch.bfloat16, out=None, stream=None):
     """The weights [D, M] that the codes stand for, as bf16 or fp32 (both exact)."""
+    if stream is None and out is None and type(w) is W4Weights and _on_gpu(w.codes):
+        r = _plain_call("dequantize", w.codes, w.exps, w.D, w.M, DTYPE.get(dtype, -1))
+        if r is not None:
+            return r
     D, M = _w4(w)
     if dtype not in (torch.float32, torch.bfloat16):
         raise TypeError(f"dtype must be torch.float32 or torch.bfloat16, got {dtype}")
@@ -813,6 +841,13 @@ def matmul_w4(A, w: W4Weights, col_bias=None, act=None, out_dtype=None, y_out=No
     ``workspace``: an optional uint8 device tensor of at least
     matmul_w4_workspace_bytes(A, M) bytes (+ up to 255 for alignment), used for
     many rows; allocated when None."""
+    if act is None:
+        act = "none" if col_bias is None else "bias"
+    if stream is None and y_out is None and workspace is None and _on_gpu(A) and type(w) is W4Weights:
+        r = _plain_call("w4", A, w.codes, w.exps, w.D, w.M, col_bias, ACT.get(act, -1) if isinstance(act, str) else -1,
+                        -1 if out_dtype is None else DTYPE.get(out_dtype, 9))
+        if r is not None:
+            return r
     code = _typed(A, "A", (torch.float32, torch.bfloat16, torch.float16), 2)
     D, M = _w4(w)
     N = A.shape[0]
@@ -821,7 +856,7 @@ def matmul_w4(A, w: W4Weights, col_bias=None, act=None, out_dtype=None, y_out=No
     lda = _row_stride(A)
     col_bias = _col_bias(col_bias, M)
     _same_device(A.device, weights=w.codes, col_bias=col_bias)
-    a = _act(act if act is not None else "none" if col_bias is None else "bias")
+    a = _act(act)
     if out_dtype is None:
         out_dtype = y_out.dtype if y_out is not None else torch.float32 if a == ACT["softmax"] else A.dtype
     if out_dtype not in (A.dtype, torch.float32):
@@ -877,6 +912,10 @@ def linear_xent(A, B, target, col_bias=None, loss_out=None, lse_out=None, worksp
     loss.  ``workspace``: an optional uint8 device tensor of at least
     linear_xent_workspace_bytes(N, D, M, A.dtype) bytes (+ up to 255 for
     alignment)."""
+    if stream is None and loss_out is None and lse_out is None and workspace is None and _on_gpu(A):
+        r = _plain_call("xent", A, B, target, col_bias)
+        if r is not None:
+            return r
     code, N, D, M, lda, first, col_bias = _xent_inputs(A, B, target, col_bias)
     with _device(A.device):
         loss_out = _output(loss_out, "loss_out", (N,), torch.float32, A.device)
@@ -898,6 +937,10 @@ def linear_xent_grad(A, B, target, lse, grad_loss, col_bias=None, dA_out=None, d
     grad_loss [N] fp32.  ``workspace``: an optional uint8 device tensor of at
     least linear_xent_grad_workspace_bytes(N, D, M, A.dtype) bytes (+ up to 255
     for alignment)."""
+    if stream is None and dA_out is None and dB_out is None and dbias_out is None and workspace is None and _on_gpu(A):
+        r = _plain_call("xent_grad", A, B, target, col_bias, lse, grad_loss)
+        if r is not None:
+            return r
     code, N, D, M, lda, first, col_bias = _xent_inputs(A, B, target, col_bias)
     for t, name in ((lse, "lse"), (grad_loss, "grad_loss")):
         _need(t, name, torch.float32, 1)

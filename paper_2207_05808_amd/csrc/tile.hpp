@@ -230,9 +230,15 @@ struct BigTile {
     }
   }
 
-  // 16 bytes a lane from base + off to LDS, 1 KB from `to` on (uniform)
-  static __device__ __forceinline__ void transfer(const void* base, uint32_t off, uint32_t to) {
+  // 16 bytes a lane from base + off to LDS, 1 KB from `to` on (uniform).  In
+  // assembly, since the compiler has every LDS read wait for all transfers under
+  // way that it knows of; product() waits for those that a read needs.
+  static __device__ __forceinline__ void transfer(const char* base, uint32_t off, uint32_t to) {
+#ifdef __OPTIMIZE__
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+#else   // (uniform values stay in vector registers there, which the assembly cannot take)
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base + off), lds_at<void>(to), 16, 0, 0);
+#endif
   }
 
   template <Order O>
