@@ -235,19 +235,31 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_dz_kernel(XArgs a) {
   if constexpr (sizeof(T) == 2) write_staged<T, Tl>(lds, out, a.ldz, a.ldz - it * BI, a.N - j0);
 }
 
+// The bias gradient from the row tiles' sums: 32 outputs a workgroup, the tiles
+// in 8 strands with 8 loads under way in each, the strands added in order.
 __global__ void __launch_bounds__(256) xent_dbias_kernel(const float* cpart, int64_t jtiles, int64_t ldz, int64_t n, float* out) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+  __shared__ float red[8][32];
+  const int strand = threadIdx.x >> 5, c = threadIdx.x & 31;
+  for (int64_t i0 = (int64_t)blockIdx.x * 32; i0 < n; i0 += (int64_t)gridDim.x * 32) {
+    const float* p = cpart + (i0 + c < n ? i0 + c : n - 1);
     float s = 0.0f;
-    int64_t j = 0;
-    for (; j + 8 <= jtiles; j += 8) {   // eight loads under way at a time
+    int64_t j = strand;
+    for (; j + 56 < jtiles; j += 64) {
       float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = cpart[(j + k) * ldz + i];
+      for (int k = 0; k < 8; ++k) v[k] = p[(j + 8 * k) * ldz];
 #pragma unroll
       for (int k = 0; k < 8; ++k) s += v[k];
     }
-    for (; j < jtiles; ++j) s += cpart[j * ldz + i];
-    out[i] = s;
+    for (; j < jtiles; j += 8) s += p[j * ldz];
+    red[strand][c] = s;
+    __syncthreads();
+    if (strand == 0 && i0 + c < n) {
+#pragma unroll
+      for (int k = 1; k < 8; ++k) s += red[k][c];
+      out[i0 + c] = s;
+    }
+    __syncthreads();
   }
 }
 
@@ -290,10 +302,18 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_gemm_kernel(GemmArgs a) {
 // Joins the shares of a split product, in order.
 template <class T>
 __global__ void __launch_bounds__(256) xent_join_splits_kernel(GemmArgs a) {
-  const int64_t I = a.X.rows, J = a.Y.rows;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < I * J; e += (int64_t)gridDim.x * 256) {
+  const int64_t I = a.X.rows, all = I * a.Y.rows;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
     float v = a.first ? 0.0f : a.sum[e];
-    for (int s = 0; s < a.splits; ++s) v += a.part[s * I * J + e];
+    int s = 0;
+    for (; s + 8 <= a.splits; s += 8) {   // eight loads under way at a time
+      float u[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) u[k] = a.part[(s + k) * all + e];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v += u[k];
+    }
+    for (; s < a.splits; ++s) v += a.part[s * all + e];
     if (a.last) static_cast<T*>(a.out)[e / I * a.ldo + e % I] = from_float<T>(v);
     else a.sum[e] = v;
   }
@@ -319,12 +339,14 @@ hipError_t launch_logits(XArgs& a, int64_t outputs, hipStream_t s) {
   else return launch(xent_tile_kernel<T, Tl>, Tl::LDS, a.itiles * a.jtiles, 1, Tl::NT, a, s);
 }
 
-// Rows of a logits tile: 256 (large bf16 products with whole units in A), 128,
-// or 32 where the wider ones would leave compute units without work.
+// Rows of a logits tile: 256 (large bf16 products with whole units in A), or
+// 128, 64 or 32: the widest that the rows fill and that leaves every compute
+// unit work.
 template <class T>
 int row_tile(const XArgs& a, int64_t outputs) {
   if (sizeof(T) == 2 && a.N >= 192 && direct(a.A, false) && cdiv(a.N, 256) * cdiv(outputs, 256) >= 192) return 256;
-  return cdiv(a.N, 128) * cdiv(outputs, 128) >= 256 ? 128 : 32;
+  if (a.N > 64 && cdiv(a.N, 128) * cdiv(outputs, 128) >= 256) return 128;
+  return a.N > 32 && cdiv(a.N, 64) * cdiv(outputs, 128) >= 256 ? 64 : 32;
 }
 
 template <class T, bool GRAD>
@@ -339,6 +361,8 @@ hipError_t logits(XArgs& a, int64_t outputs, int rows, bool md, hipStream_t s) {
   }
   if (rows >= 128) return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>>(a, outputs, s)
                              : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 128, 2, 2>>(a, outputs, s);
+  if (rows == 64) return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 64, 4, 1>>(a, outputs, s)
+                            : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 64, 4, 1>>(a, outputs, s);
   return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 32, 4, 1>>(a, outputs, s)
             : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 32, 4, 1>>(a, outputs, s);
 }
@@ -412,7 +436,7 @@ hipError_t grad(XArgs a, bool md, void* dA, void* dB, float* dbias, char* ws, hi
     z.ldz = up(n, 64);
     hipError_t e = logits<T, true>(z, z.ldz, row_tile<T>(a, g.p), md, s);
     if (e != hipSuccess) return e;
-    const int64_t b = cdiv(n, 256);
+    const int64_t b = cdiv(n, 32);
     hipLaunchKernelGGL(xent_dbias_kernel, dim3((unsigned)(b < 4096 ? b : 4096)), dim3(256), 0, s, z.cpart, z.jtiles, z.ldz, n, dbias + m0);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const Operand zk{z.dz, z.ldz, a.N, a.N}, zi{z.dz, z.ldz, n, z.ldz};

@@ -47,6 +47,7 @@ struct Tile {
   static constexpr int XB = BI * BK * 2, YB = BJ * BK * 2;               // bytes of one part's LDS tile
   static constexpr int STAGE = P * (XB + YB);
   static constexpr int LDS = 2 * STAGE;
+  static constexpr int AHEAD = 3;   // steps loaded ahead into registers: memory takes longer than a step's products
   static_assert(XU * CH * NT == BI * BK && YU * CH * NT == BJ * BK && MI * WI * 32 == BI && NJ * WJ * 32 == BJ, "tile");
   typedef f32x16 Acc[MI][NJ];
 
@@ -79,13 +80,28 @@ struct Tile {
     }
   }
 
+  // A step's units of this thread.  Where the whole step lies in the operand's
+  // memory, rows past its end are read as what stands there (along k: as its
+  // last row): they reach only results that are not written.  Elsewhere, and for
+  // k past the end, zeros take their place.
   template <Order O, int B, int U>
-  static __device__ __forceinline__ void load(const Operand& o, int64_t r0, int64_t k0, int64_t kend, u32x4 (&v)[U], int first = 0) {
+  static __device__ __forceinline__ void load(const Operand& o, int64_t r0, int64_t k0, int64_t kend, u32x4 (&v)[U]) {
+    const T* base = static_cast<const T*>(o.p) + (O == kAlongK ? r0 * o.ld + k0 : k0 * o.ld + r0);
+    if (k0 + BK <= kend && (O == kAlongK || (k0 + BK - 1) * o.ld + r0 + B <= (kend - 1) * o.ld + o.rows)) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        int r, k;
+        unit<O, B>(threadIdx.x + i * NT, r, k);
+        const int64_t last = o.rows - 1 - r0;
+        v[i] = load16(base + (O == kAlongK ? (r < last ? r : last) * o.ld + k : k * o.ld + r));
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       int r, k;
-      unit<O, B>(threadIdx.x + (first + i) * NT, r, k);
-      const T* p = static_cast<const T*>(o.p) + (O == kAlongK ? (r0 + r) * o.ld + (k0 + k) : (k0 + k) * o.ld + (r0 + r));
+      unit<O, B>(threadIdx.x + i * NT, r, k);
+      const T* p = base + (O == kAlongK ? r * o.ld + k : k * o.ld + r);
       // elements of the unit inside the matrix
       const bool in = r0 + r < o.rows && k0 + k < kend;
       const int64_t left = !in ? 0 : O == kAlongK ? kend - (k0 + k) : o.rows - (r0 + r);
@@ -104,11 +120,11 @@ struct Tile {
   }
 
   template <Order O, int B, int U>
-  static __device__ __forceinline__ void store(uint32_t lds, const u32x4 (&v)[U], int first = 0) {
+  static __device__ __forceinline__ void store(uint32_t lds, const u32x4 (&v)[U]) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       int r, k;
-      unit<O, B>(threadIdx.x + (first + i) * NT, r, k);
+      unit<O, B>(threadIdx.x + i * NT, r, k);
       const uint32_t p = lds + at<O, B>(r, k);
       if constexpr (P == 1) {
         *lds_at<u32x4>(p) = v[i];
@@ -143,47 +159,55 @@ struct Tile {
                                                  int64_t kend, uint32_t lds, Acc& acc) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int bi = (wave / WJ) * 32 * MI, bj = (wave % WJ) * 32 * NJ;
-    u32x4 xv[XU], yv[YU];
+    u32x4 xv[AHEAD][XU], yv[AHEAD][YU];
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
       for (int nj = 0; nj < NJ; ++nj)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[mi][nj][r] = 0.0f;
-    load<OX, BI>(X, i0, k0, kend, xv);
-    load<OY, BJ>(Y, j0, k0, kend, yv);
-    int64_t back = 0;   // k of Y less k of X
+    int64_t kx = k0, ky = k0;   // the next step to load
+    auto fetch = [&](int u) {
+      if (ky >= kend) return;
+      load<OX, BI>(X, i0, kx, X.wrap ? X.wrap : kend, xv[u]);
+      load<OY, BJ>(Y, j0, ky, kend, yv[u]);
+      kx += BK;
+      ky += BK;
+      if (X.wrap && kx == X.wrap) kx = 0;
+    };
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) fetch(u);
     uint32_t buf = lds;
-    for (int64_t k = k0; k < kend; k += BK) {
-      store<OX, BI>(buf, xv);
-      store<OY, BJ>(buf + P * XB, yv);
-      if (k + BK < kend) {
-        if (X.wrap && k + BK - back == X.wrap) back += X.wrap;
-        load<OX, BI>(X, i0, k + BK - back, kend - back, xv);
-        load<OY, BJ>(Y, j0, k + BK, kend, yv);
-      }
-      lds_only_barrier();   // a wavefront writes this buffer again only after the next barrier
+    for (int64_t k1 = k0; k1 < kend; k1 += AHEAD * BK) {
 #pragma unroll
-      for (int ks = 0; ks < BK / 16; ++ks) {
-        bf16x8 x[P][MI], y[P][NJ];
+      for (int u = 0; u < AHEAD; ++u) {
+        if (k1 + u * BK >= kend) break;
+        store<OX, BI>(buf, xv[u]);
+        store<OY, BJ>(buf + P * XB, yv[u]);
+        fetch(u);
+        lds_only_barrier();   // a wavefront writes this buffer again only after the next barrier
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
+        for (int ks = 0; ks < BK / 16; ++ks) {
+          bf16x8 x[P][MI], y[P][NJ];
 #pragma unroll
-          for (int mi = 0; mi < MI; ++mi) x[p][mi] = frag<OX, BI>(buf + p * XB, bi + 32 * mi, ks, lane);
+          for (int p = 0; p < P; ++p) {
 #pragma unroll
-          for (int nj = 0; nj < NJ; ++nj) y[p][nj] = frag<OY, BJ>(buf + P * XB + p * YB, bj + 32 * nj, ks, lane);
+            for (int mi = 0; mi < MI; ++mi) x[p][mi] = frag<OX, BI>(buf + p * XB, bi + 32 * mi, ks, lane);
+#pragma unroll
+            for (int nj = 0; nj < NJ; ++nj) y[p][nj] = frag<OY, BJ>(buf + P * XB + p * YB, bj + 32 * nj, ks, lane);
+          }
+#pragma unroll
+          for (int sum = P - 1; sum >= 0; --sum)   // smallest terms first
+#pragma unroll
+            for (int p = 0; p <= sum; ++p)
+#pragma unroll
+              for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                for (int nj = 0; nj < NJ; ++nj)
+                  acc[mi][nj] = multiply_add<T>(x[p][mi], y[sum - p][nj], acc[mi][nj]);
         }
-#pragma unroll
-        for (int sum = P - 1; sum >= 0; --sum)   // smallest terms first
-#pragma unroll
-          for (int p = 0; p <= sum; ++p)
-#pragma unroll
-            for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-              for (int nj = 0; nj < NJ; ++nj)
-                acc[mi][nj] = multiply_add<T>(x[p][mi], y[sum - p][nj], acc[mi][nj]);
+        buf = buf == lds ? lds + STAGE : lds;
       }
-      buf = buf == lds ? lds + STAGE : lds;
     }
     __syncthreads();   // the buffers are free
   }

@@ -165,52 +165,123 @@ struct QArgs {
   uint8_t* codes; uint8_t* exps;
 };
 
-// One wavefront per packed block.  Lane (quarter, column) holds the 32 weights
-// that it will write: 8 rows of each of the block's four groups.
-template <class T>
+// The codes of 8 weights of a group with exponent e (0 where the group is not
+// finite), and what the exponent byte of a group is.
+__device__ __forceinline__ uint32_t codes_of(const float (&v)[8], int e, bool bad) {
+  uint32_t word = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float t = ldexpf(__builtin_fabsf(v[i]), -e);   // (exact, or far below the first edge)
+    uint32_t q = (t > 0.25f) + (t >= 0.75f) + (t > 1.25f) + (t >= 1.75f) + (t > 2.5f) + (t >= 3.5f) + (t > 5.0f);
+    q = bad ? 0 : q && v[i] < 0.0f ? q + 8 : q;
+    word |= q << (4 * i);
+  }
+  return word;
+}
+// the smallest e with top <= 6 2^e: top = f 2^x, 1/2 <= f < 1, and 6 2^e = 3/4 2^(e + 3)
+__device__ __forceinline__ int exponent_of(float top, bool inside) {
+  int x = 0;
+  const float f = frexpf(top, &x);
+  const int e = f <= 0.75f ? x - 3 : x - 2;
+  return top == 0.0f ? (inside ? -120 : 0) : e < -120 ? -120 : e > 125 ? 125 : e;
+}
+
+// B with its rows d contiguous (stride_d 1), or any strides.  One wavefront per
+// packed block; lane (quarter, column) holds the 32 weights that it will write,
+// 8 consecutive rows of each of the block's four groups: 16 or 32 bytes a load,
+// a column's 128 rows in whole lines.
+template <class T, bool DENSE>
 __global__ void __launch_bounds__(256) w4_quantize_kernel(QArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, quarter = lane >> 4;
   const int64_t blocks = (int64_t)a.nk * a.nm;
   for (int64_t b = (int64_t)blockIdx.x * 4 + wave; b < blocks; b += (int64_t)gridDim.x * 4) {
-    const int mb = (int)(b % a.nm), kb = (int)(b / a.nm);   // neighbours share the lines of B's rows
+    // neighbours: the next rows of the same columns, or (other strides) the next columns
+    const int mb = (int)(DENSE ? b / a.nk : b % a.nm), kb = (int)(DENSE ? b % a.nk : b / a.nm);
     const int m = mb * kWM + col;
     const T* src = static_cast<const T*>(a.B) + m * a.sm;
-    u32x4 word = {0, 0, 0, 0};
+    float v[4][8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = kb * kWK + 32 * j + 8 * quarter;
+      if (DENSE && m < a.M && d + 8 <= a.D) {
+        if constexpr (sizeof(T) == 4) {
+          const u32x4 x = load16(src + d), y = load16(src + d + 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { v[j][i] = __uint_as_float(x[i]); v[j][4 + i] = __uint_as_float(y[i]); }
+        } else {
+          const u32x4 x = load16(src + d);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[j][i] = to_float(T{(uint16_t)(x[i >> 1] >> (16 * (i & 1)))});
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] = d + i < a.D && m < a.M ? to_float(src[(d + i) * a.sd]) : 0.0f;
+      }
+    }
+    u32x4 word;
     uint32_t exps = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      float v[8], top = 0.0f;
-      bool odd = false;   // not finite
+      float top = 0.0f;
+      int odd = 0;   // not finite
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int d = kb * kWK + 32 * j + 8 * quarter + i;
-        v[i] = d < a.D && m < a.M ? to_float(src[d * a.sd]) : 0.0f;
-        top = __builtin_fmaxf(top, __builtin_fabsf(v[i]));
-        odd = odd || !(__builtin_fabsf(v[i]) < __builtin_inff());
+        top = __builtin_fmaxf(top, __builtin_fabsf(v[j][i]));
+        odd |= !(__builtin_fabsf(v[j][i]) < __builtin_inff());
       }
       top = __builtin_fmaxf(top, __shfl_xor(top, 16));
       top = __builtin_fmaxf(top, __shfl_xor(top, 32));
-      int bad = odd;
-      bad |= __shfl_xor(bad, 16);
-      bad |= __shfl_xor(bad, 32);
-      // the smallest e with top <= 6 2^e: top = f 2^x, 1/2 <= f < 1, and 6 2^e = 3/4 2^(e + 3)
-      int x = 0;
-      const float f = frexpf(top, &x);
-      int e = f <= 0.75f ? x - 3 : x - 2;
-      e = top == 0.0f ? (kb * kWK + 32 * j < a.D && m < a.M ? -120 : 0) : e < -120 ? -120 : e > 125 ? 125 : e;
-      exps |= (uint32_t)(bad ? 255 : e + 127) << (8 * j);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float t = ldexpf(__builtin_fabsf(v[i]), -e);   // (exact, or far below the first edge)
-        uint32_t q = (t > 0.25f) + (t >= 0.75f) + (t > 1.25f) + (t >= 1.75f) + (t > 2.5f) + (t >= 3.5f) + (t > 5.0f);
-        q = bad ? 0 : q && v[i] < 0.0f ? q + 8 : q;
-        word[j] |= q << (4 * i);
-      }
+      odd |= __shfl_xor(odd, 16);
+      odd |= __shfl_xor(odd, 32);
+      const int e = exponent_of(top, kb * kWK + 32 * j < a.D && m < a.M);
+      exps |= (uint32_t)(odd ? 255 : e + 127) << (8 * j);
+      word[j] = codes_of(v[j], e, odd);
     }
     const int64_t at = (int64_t)mb * a.nk + kb;
     reinterpret_cast<u32x4*>(a.codes)[at * 64 + lane] = word;
     if (quarter == 0) reinterpret_cast<uint32_t*>(a.exps)[at * 16 + col] = exps;
+  }
+}
+
+// B with its columns contiguous (stride_m 1): a wavefront takes 64 columns, a
+// lane one of them, so that every load is 128 or 256 bytes of a row and a
+// group's maximum stays in its lane.
+template <class T>
+__global__ void __launch_bounds__(256) w4_quantize_rows_kernel(QArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15;
+  const int64_t strips = (a.nm + 3) / 4, blocks = (int64_t)a.nk * strips;
+  for (int64_t b = (int64_t)blockIdx.x * 4 + wave; b < blocks; b += (int64_t)gridDim.x * 4) {
+    const int kb = (int)(b / strips), m = (int)(b % strips) * 64 + lane, mb = m >> 4;
+    const T* src = static_cast<const T*>(a.B) + m;
+    u32x4 word[4];
+    uint32_t exps = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float v[4][8], top = 0.0f;
+      bool odd = false;
+      const int d = kb * kWK + 32 * j;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[q][i] = d + 8 * q + i < a.D && m < a.M ? to_float(src[(d + 8 * q + i) * a.sd]) : 0.0f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          top = __builtin_fmaxf(top, __builtin_fabsf(v[q][i]));
+          odd = odd || !(__builtin_fabsf(v[q][i]) < __builtin_inff());
+        }
+      const int e = exponent_of(top, d < a.D && m < a.M);
+      exps |= (uint32_t)(odd ? 255 : e + 127) << (8 * j);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) word[q][j] = codes_of(v[q], e, odd);
+    }
+    if (mb >= a.nm) continue;
+    const int64_t at = (int64_t)mb * a.nk + kb;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) reinterpret_cast<u32x4*>(a.codes)[at * 64 + q * 16 + col] = word[q];
+    reinterpret_cast<uint32_t*>(a.exps)[at * 16 + col] = exps;
   }
 }
 
@@ -219,26 +290,33 @@ struct DArgs {
   void* B;   // [D][M]
 };
 
+// A wavefront takes 64 columns of a block of rows, a lane one of them: every
+// store is 128 or 256 bytes of a row.
 template <class T>
 __global__ void __launch_bounds__(256) w4_dequantize_kernel(DArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int col = lane & 15, quarter = lane >> 4;
-  const int64_t blocks = (int64_t)a.nk * a.nm;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15;
+  const int64_t strips = (a.nm + 3) / 4, blocks = (int64_t)a.nk * strips;
   for (int64_t b = (int64_t)blockIdx.x * 4 + wave; b < blocks; b += (int64_t)gridDim.x * 4) {
-    const int mb = (int)(b % a.nm), kb = (int)(b / a.nm);
-    const int m = mb * kWM + col;
-    const int64_t at = (int64_t)mb * a.nk + kb;
-    const u32x4 w = reinterpret_cast<const u32x4*>(a.codes)[at * 64 + lane];
+    const int kb = (int)(b / strips), m = (int)(b % strips) * 64 + lane;
+    if (m >= a.M) continue;
+    const int64_t at = (int64_t)(m >> 4) * a.nk + kb;
     const uint32_t e = reinterpret_cast<const uint32_t*>(a.exps)[at * 16 + col];
+    u32x4 w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bf16x8 v = unpack8(w[j], scale_of(e, j));
+    for (int q = 0; q < 4; ++q) w[q] = reinterpret_cast<const u32x4*>(a.codes)[at * 64 + q * 16 + col];
+    T* out = static_cast<T*>(a.B) + (int64_t)kb * kWK * a.M + m;
+    const int left = a.D - kb * kWK;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int d = kb * kWK + 32 * j + 8 * quarter + i;
-        if (d < a.D && m < a.M) static_cast<T*>(a.B)[(int64_t)d * a.M + m] = from_float<T>((float)v[i]);
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const bf16x8 v = unpack8(w[q][j], scale_of(e, j));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int d = 32 * j + 8 * q + i;
+          if (d < left) out[(int64_t)d * a.M] = from_float<T>((float)v[i]);
+        }
       }
-    }
   }
 }
 
@@ -377,6 +455,15 @@ int blocks_for(int64_t waves, int per) {
   return (int)(b < most ? b : most);
 }
 
+template <class T>
+hipError_t launch_quantize(const QArgs& a, hipStream_t s) {
+  const int64_t blocks = (int64_t)a.nk * a.nm;
+  if (a.sm == 1 && a.sd != 1) hipLaunchKernelGGL((w4_quantize_rows_kernel<T>), dim3(blocks_for((int64_t)a.nk * ((a.nm + 3) / 4), 4)), dim3(256), 0, s, a);
+  else if (a.sd == 1) hipLaunchKernelGGL((w4_quantize_kernel<T, true>), dim3(blocks_for(blocks, 4)), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((w4_quantize_kernel<T, false>), dim3(blocks_for(blocks, 4)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
 template <class T, class Y, int RT>
 hipError_t launch_rows(const WArgs& a, hipStream_t stream) {
   const int waves = a.nk < 8 ? a.nk : 8;
@@ -489,12 +576,8 @@ int maddness_quantize_w4(const void* B, int32_t dtype, int32_t D, int32_t M, int
   if (dtype < MADDNESS_F32 || dtype > MADDNESS_F16) return MADDNESS_EINVAL;
   if (!aligned(B, dtype == MADDNESS_F32 ? 4 : 2) || !aligned(codes_out, 16) || !aligned(exps_out, 4)) return MADDNESS_EINVAL;
   QArgs a{B, stride_d, stride_m, D, M, (int)(((int64_t)D + kWK - 1) / kWK), (int)(((int64_t)M + kWM - 1) / kWM), codes_out, exps_out};
-  const dim3 grid(blocks_for((int64_t)a.nk * a.nm, 4));
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (dtype == MADDNESS_F32) hipLaunchKernelGGL((w4_quantize_kernel<float>), grid, dim3(256), 0, s, a);
-  else if (dtype == MADDNESS_BF16) hipLaunchKernelGGL((w4_quantize_kernel<Bf16>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((w4_quantize_kernel<F16>), grid, dim3(256), 0, s, a);
-  return status_from(hipGetLastError());
+  return status_from(dtype == MADDNESS_F32 ? launch_quantize<float>(a, s) : dtype == MADDNESS_BF16 ? launch_quantize<Bf16>(a, s) : launch_quantize<F16>(a, s));
 }
 
 int maddness_dequantize_w4(const uint8_t* codes, const uint8_t* exps, int32_t D, int32_t M, void* B_out, int32_t dtype,
@@ -503,7 +586,7 @@ int maddness_dequantize_w4(const uint8_t* codes, const uint8_t* exps, int32_t D,
   if (dtype != MADDNESS_F32 && dtype != MADDNESS_BF16) return MADDNESS_EINVAL;
   if (!aligned(B_out, dtype == MADDNESS_F32 ? 4 : 2) || !aligned(codes, 16) || !aligned(exps, 4)) return MADDNESS_EINVAL;
   DArgs a{codes, exps, D, M, (int)(((int64_t)D + kWK - 1) / kWK), (int)(((int64_t)M + kWM - 1) / kWM), B_out};
-  const dim3 grid(blocks_for((int64_t)a.nk * a.nm, 4));
+  const dim3 grid(blocks_for((int64_t)a.nk * ((a.nm + 3) / 4), 4));
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (dtype == MADDNESS_F32) hipLaunchKernelGGL((w4_dequantize_kernel<float>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((w4_dequantize_kernel<Bf16>), grid, dim3(256), 0, s, a);
