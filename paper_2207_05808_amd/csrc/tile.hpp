@@ -80,23 +80,35 @@ struct Tile {
     }
   }
 
-  // A step's units of this thread.  Where the whole step lies in the operand's
-  // memory, rows past its end are read as what stands there (along k: as its
-  // last row): they reach only results that are not written.  Elsewhere, and for
-  // k past the end, zeros take their place.
+  // The leading steps of k0 .. kend that lie in the operand's memory whole: rows
+  // past its end are read as what stands there (along k: as its last row), and
+  // reach only results that are not written.
+  template <Order O, int B>
+  static __device__ __forceinline__ int64_t whole_steps(const Operand& o, int64_t r0, int64_t k0, int64_t kend) {
+    const int64_t full = (kend - k0) / BK;
+    if (O == kAlongK) return full;
+    // step s: (k0 + s BK + BK - 1) ld + r0 + B <= (kend - 1) ld + rows
+    const int64_t over = r0 + B - o.rows, lines = over > 0 ? (over + o.ld - 1) / o.ld : 0, n = (kend - k0 - lines) / BK;
+    return kend - k0 < lines ? 0 : n < full ? n : full;
+  }
+
+  // units of such a step
+  template <Order O, int B, int U>
+  static __device__ __forceinline__ void load_whole(const Operand& o, int64_t r0, int64_t k0, u32x4 (&v)[U]) {
+    const T* base = static_cast<const T*>(o.p) + (O == kAlongK ? r0 * o.ld + k0 : k0 * o.ld + r0);
+    const int64_t last = o.rows - 1 - r0;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      int r, k;
+      unit<O, B>(threadIdx.x + i * NT, r, k);
+      v[i] = load16(base + (O == kAlongK ? (r < last ? r : last) * o.ld + k : k * o.ld + r));
+    }
+  }
+
+  // units of any step, zeros past the matrix and past kend
   template <Order O, int B, int U>
   static __device__ __forceinline__ void load(const Operand& o, int64_t r0, int64_t k0, int64_t kend, u32x4 (&v)[U]) {
     const T* base = static_cast<const T*>(o.p) + (O == kAlongK ? r0 * o.ld + k0 : k0 * o.ld + r0);
-    if (k0 + BK <= kend && (O == kAlongK || (k0 + BK - 1) * o.ld + r0 + B <= (kend - 1) * o.ld + o.rows)) {
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        int r, k;
-        unit<O, B>(threadIdx.x + i * NT, r, k);
-        const int64_t last = o.rows - 1 - r0;
-        v[i] = load16(base + (O == kAlongK ? (r < last ? r : last) * o.ld + k : k * o.ld + r));
-      }
-      return;
-    }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       int r, k;
@@ -166,48 +178,66 @@ struct Tile {
       for (int nj = 0; nj < NJ; ++nj)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[mi][nj][r] = 0.0f;
-    int64_t kx = k0, ky = k0;   // the next step to load
-    auto fetch = [&](int u) {
-      if (ky >= kend) return;
-      load<OX, BI>(X, i0, kx, X.wrap ? X.wrap : kend, xv[u]);
-      load<OY, BJ>(Y, j0, ky, kend, yv[u]);
-      kx += BK;
-      ky += BK;
-      if (X.wrap && kx == X.wrap) kx = 0;
-    };
+    auto multiply = [&](uint32_t buf) {
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) fetch(u);
-    uint32_t buf = lds;
-    for (int64_t k1 = k0; k1 < kend; k1 += AHEAD * BK) {
+      for (int ks = 0; ks < BK / 16; ++ks) {
+        bf16x8 x[P][MI], y[P][NJ];
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        if (k1 + u * BK >= kend) break;
-        store<OX, BI>(buf, xv[u]);
-        store<OY, BJ>(buf + P * XB, yv[u]);
-        fetch(u);
-        lds_only_barrier();   // a wavefront writes this buffer again only after the next barrier
+        for (int p = 0; p < P; ++p) {
 #pragma unroll
-        for (int ks = 0; ks < BK / 16; ++ks) {
-          bf16x8 x[P][MI], y[P][NJ];
+          for (int mi = 0; mi < MI; ++mi) x[p][mi] = frag<OX, BI>(buf + p * XB, bi + 32 * mi, ks, lane);
 #pragma unroll
-          for (int p = 0; p < P; ++p) {
-#pragma unroll
-            for (int mi = 0; mi < MI; ++mi) x[p][mi] = frag<OX, BI>(buf + p * XB, bi + 32 * mi, ks, lane);
-#pragma unroll
-            for (int nj = 0; nj < NJ; ++nj) y[p][nj] = frag<OY, BJ>(buf + P * XB + p * YB, bj + 32 * nj, ks, lane);
-          }
-#pragma unroll
-          for (int sum = P - 1; sum >= 0; --sum)   // smallest terms first
-#pragma unroll
-            for (int p = 0; p <= sum; ++p)
-#pragma unroll
-              for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-                for (int nj = 0; nj < NJ; ++nj)
-                  acc[mi][nj] = multiply_add<T>(x[p][mi], y[sum - p][nj], acc[mi][nj]);
+          for (int nj = 0; nj < NJ; ++nj) y[p][nj] = frag<OY, BJ>(buf + P * XB + p * YB, bj + 32 * nj, ks, lane);
         }
-        buf = buf == lds ? lds + STAGE : lds;
+#pragma unroll
+        for (int sum = P - 1; sum >= 0; --sum)   // smallest terms first
+#pragma unroll
+          for (int p = 0; p <= sum; ++p)
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+              for (int nj = 0; nj < NJ; ++nj)
+                acc[mi][nj] = multiply_add<T>(x[p][mi], y[sum - p][nj], acc[mi][nj]);
       }
+    };
+    if (k0 >= kend) return;
+    // whole steps, loaded AHEAD of their use without a branch (so that a use
+    // waits for its own step's loads alone; past the last, that one again)
+    const int64_t sx = whole_steps<OX, BI>(X, i0, k0, kend), sy = whole_steps<OY, BJ>(Y, j0, k0, kend), whole = sx < sy ? sx : sy;
+    uint32_t buf = lds;
+    if (whole > 0) {
+      int64_t kx = k0, ky = k0, left = whole;   // the next step to load
+      auto fetch = [&](int u) {
+        load_whole<OX, BI>(X, i0, kx, xv[u]);
+        load_whole<OY, BJ>(Y, j0, ky, yv[u]);
+        const int64_t d = --left > 0 ? BK : 0;
+        kx += d;
+        ky += d;
+        kx = d && X.wrap && kx == X.wrap ? 0 : kx;
+      };
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) fetch(u);
+      for (int64_t s = 0; s < whole; s += AHEAD) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+          if (s + u >= whole) break;
+          store<OX, BI>(buf, xv[u]);
+          store<OY, BJ>(buf + P * XB, yv[u]);
+          fetch(u);
+          lds_only_barrier();   // a wavefront writes this buffer again only after the next barrier
+          multiply(buf);
+          buf = buf == lds ? lds + STAGE : lds;
+        }
+      }
+    }
+    for (int64_t k = k0 + whole * BK; k < kend; k += BK) {   // what is left, with checks (X.wrap leaves none)
+      load<OX, BI>(X, i0, k, kend, xv[0]);
+      load<OY, BJ>(Y, j0, k, kend, yv[0]);
+      store<OX, BI>(buf, xv[0]);
+      store<OY, BJ>(buf + P * XB, yv[0]);
+      lds_only_barrier();
+      multiply(buf);
+      buf = buf == lds ? lds + STAGE : lds;
     }
     __syncthreads();   // the buffers are free
   }
@@ -308,10 +338,14 @@ struct BigTile {
     Stream<OX> sx;
     Stream<OY> sy;
     u32x4 held[STAGED_X ? U : 1];
+    const int64_t whole_x = STAGED_X && steps > 0 ? Small::template whole_steps<OX, 256>(X, i0, k0, kend) : 0;
     if constexpr (!STAGED_X) sx.init(X, i0, k0, lds);
     sy.init(Y, j0, k0, lds);
     auto fetch = [&](int s) {   // a staged step to registers
-      if constexpr (STAGED_X) Small::template load<OX, 256, U>(X, i0, k0 + (int64_t)s * BK, kend, held);
+      if constexpr (STAGED_X) {
+        if (s < whole_x) Small::template load_whole<OX, 256, U>(X, i0, k0 + (int64_t)s * BK, held);
+        else Small::template load<OX, 256, U>(X, i0, k0 + (int64_t)s * BK, kend, held);
+      }
     };
     auto put = [&](uint32_t at) {   // and from there to its slot
       if constexpr (STAGED_X) Small::template store<OX, 256, U>(lds + at, held);
