@@ -43,22 +43,22 @@ __device__ __forceinline__ int target_at(int64_t t, int64_t M, int64_t i0) {
 
 template <class T, class Tl>
 __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
-  constexpr int BI = Tl::BI, BJ = Tl::BJ, WI = Tl::WI, WJ = Tl::WJ;
+  constexpr int BI = Tl::BI, BJ = Tl::BJ, WI = Tl::WI;
   extern __shared__ __align__(16) char lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
   int64_t it, jt;
   tile_of(blockIdx.x, a.itiles, a.jtiles, it, jt);
   const int64_t i0 = it * BI, j0 = jt * BJ;
   typename Tl::Acc acc;
   Tl::product(a.W, a.A, i0, j0, 0, a.D, lds_address(lds), acc);
-  const int bi = (wave / WJ) * 32 * Tl::MI, bj = (wave % WJ) * 32 * Tl::NJ;
+  const int bi = Tl::base_i(), bj = Tl::base_j();
   float b[Tl::MI][16];
   load_bias<Tl>(b, a.bias, i0 + bi, a.M);
   float2* red = reinterpret_cast<float2*>(lds);   // [WI][BJ]
 #pragma unroll
   for (int nj = 0; nj < Tl::NJ; ++nj) {
     const int64_t j = j0 + bj + 32 * nj + (lane & 31);
-    const int t = j < a.N ? target_at(a.target[j], a.M, i0 + bi) : -1;
+    const int t = j < a.N && Tl::lead() ? target_at(a.target[j], a.M, i0 + bi) : -1;
     float top = -__builtin_inff();
 #pragma unroll
     for (int mi = 0; mi < Tl::MI; ++mi) {
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) sum += exp_of(acc[mi][nj][r] + b[mi][r] - base);
     sum += __shfl_xor(sum, 32);
-    if (lane < 32) red[(wave / WJ) * BJ + bj + 32 * nj + lane] = make_float2(top, sum);
+    if (lane < 32 && Tl::lead()) red[Tl::wi() * BJ + bj + 32 * nj + lane] = make_float2(top, sum);
   }
   __syncthreads();
   for (int j = threadIdx.x; j < BJ; j += Tl::NT) {
@@ -121,8 +121,7 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2* part, cons
 // Adds what a tile of 32-bit sums (as write_tile writes them) holds.
 template <class Tl>
 __device__ __forceinline__ void add_tile(typename Tl::Acc& acc, const float* sum, int64_t ld, int64_t I, int64_t J) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int bi = (wave / Tl::WJ) * 32 * Tl::MI, bj = (wave % Tl::WJ) * 32 * Tl::NJ;
+  const int lane = threadIdx.x & 63, bi = Tl::base_i(), bj = Tl::base_j();
 #pragma unroll
   for (int nj = 0; nj < Tl::NJ; ++nj) {
     const int j = bj + 32 * nj + (lane & 31);
@@ -173,13 +172,13 @@ template <class T, class Tl>
 __global__ void __launch_bounds__(Tl::NT, 1) xent_dz_kernel(XArgs a) {
   constexpr int BI = Tl::BI, BJ = Tl::BJ, WJ = Tl::WJ;
   extern __shared__ __align__(16) char lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
   int64_t it, jt;
   tile_of(blockIdx.x, a.itiles, a.jtiles, it, jt);
   const int64_t i0 = a.m0 + it * BI, j0 = jt * BJ;
   typename Tl::Acc acc;
   Tl::product(a.W, a.A, i0, j0, 0, a.D, lds_address(lds), acc);
-  const int bi = (wave / WJ) * 32 * Tl::MI, bj = (wave % WJ) * 32 * Tl::NJ;
+  const int bi = Tl::base_i(), bj = Tl::base_j();
   float b[Tl::MI][16], cols[Tl::MI][16];
   load_bias<Tl>(b, a.bias, i0 + bi, a.M);
   T* out = static_cast<T*>(a.dz) + j0 * a.ldz + it * BI;
@@ -210,6 +209,7 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_dz_kernel(XArgs a) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int i = bi + 32 * mi + entry_row(4 * q, lane);
+        if (!Tl::lead()) continue;
         if constexpr (sizeof(T) == 2) stage4<T, Tl>(lds, i, (int)(j - j0), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
         else if (j < a.N) write4(out + (j - j0) * a.ldz + i, a.ldz - it * BI - i, (f32x4){v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]});
       }
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_dz_kernel(XArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
       const float s = sums32(cols[mi][r], cols[mi][r + 1]);
-      if ((lane & 15) == 0) red[(wave % WJ) * BI + bi + 32 * mi + entry_row(r, lane) + ((lane >> 4) & 1)] = s;
+      if ((lane & 15) == 0 && Tl::lead()) red[Tl::wj() * BI + bi + 32 * mi + entry_row(r, lane) + ((lane >> 4) & 1)] = s;
     }
   __syncthreads();
   for (int i = threadIdx.x; i < BI; i += Tl::NT) {

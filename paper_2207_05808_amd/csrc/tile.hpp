@@ -33,15 +33,30 @@ struct Operand {
   int64_t wrap;   // k after which the operand begins again (a multiple of 64; 0: it does not)
 };
 
-// A tile of BI x BJ results of one workgroup of WI x WJ wavefronts, k in steps
-// of BK through two LDS buffers.
-template <class T, Order OX, Order OY, int BI_, int BJ_, int WI_, int WJ_, int BK_ = sizeof(T) == 2 ? 64 : 32>
-struct Tile {
+// Where a tile's wavefronts stand: WI x WJ of them side by side, WK times over
+// (each time for other k of a step; all WK end with the whole sums, and the
+// first of them writes).
+template <int WI, int WJ, int WK, int MI, int NJ>
+struct Waves {
+  static __device__ __forceinline__ int wave() { return (threadIdx.x >> 6) % (WI * WJ); }
+  static __device__ __forceinline__ int wk() { return WK == 1 ? 0 : (threadIdx.x >> 6) / (WI * WJ); }
+  static __device__ __forceinline__ bool lead() { return WK == 1 || wk() == 0; }
+  static __device__ __forceinline__ int wi() { return wave() / WJ; }
+  static __device__ __forceinline__ int wj() { return wave() % WJ; }
+  static __device__ __forceinline__ int base_i() { return wi() * 32 * MI; }
+  static __device__ __forceinline__ int base_j() { return wj() * 32 * NJ; }
+};
+
+// A tile of BI x BJ results of one workgroup, k in steps of BK through two LDS
+// buffers.
+template <class T, Order OX, Order OY, int BI_, int BJ_, int WI_, int WJ_, int BK_ = sizeof(T) == 2 ? 64 : 32, int WK = 1>
+struct Tile : Waves<WI_, WJ_, WK, BI_ / WI_ / 32, BJ_ / WJ_ / 32> {
+  typedef Waves<WI_, WJ_, WK, BI_ / WI_ / 32, BJ_ / WJ_ / 32> Place;
   static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_;
   static constexpr int P = sizeof(T) == 2 ? 1 : Parts<T>::n;   // 16-bit types as they are
   static constexpr int BK = BK_;
   static constexpr int CH = 16 / sizeof(T);          // elements of a 16-byte unit
-  static constexpr int NT = WI * WJ * 64;
+  static constexpr int NT = WI * WJ * WK * 64;
   static constexpr int MI = BI / WI / 32, NJ = BJ / WJ / 32;
   static constexpr int XU = BI * BK / CH / NT, YU = BJ * BK / CH / NT;   // units a thread moves per step
   static constexpr int XB = BI * BK * 2, YB = BJ * BK * 2;               // bytes of one part's LDS tile
@@ -169,8 +184,7 @@ struct Tile {
   // column j = base_j + 32 nj + lane % 32
   static __device__ __forceinline__ void product(const Operand& X, const Operand& Y, int64_t i0, int64_t j0, int64_t k0,
                                                  int64_t kend, uint32_t lds, Acc& acc) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int bi = (wave / WJ) * 32 * MI, bj = (wave % WJ) * 32 * NJ;
+    const int lane = threadIdx.x & 63, bi = Place::base_i(), bj = Place::base_j();
     u32x4 xv[AHEAD][XU], yv[AHEAD][YU];
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi)
@@ -180,7 +194,8 @@ struct Tile {
         for (int r = 0; r < 16; ++r) acc[mi][nj][r] = 0.0f;
     auto multiply = [&](uint32_t buf) {
 #pragma unroll
-      for (int ks = 0; ks < BK / 16; ++ks) {
+      for (int n = 0; n < BK / 16 / WK; ++n) {
+        const int ks = n * WK + Place::wk();
         bf16x8 x[P][MI], y[P][NJ];
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -240,6 +255,29 @@ struct Tile {
       buf = buf == lds ? lds + STAGE : lds;
     }
     __syncthreads();   // the buffers are free
+    if constexpr (WK > 1) {   // the sums over k of all WK, in order
+      static_assert(WK * BI * BJ * 4 <= LDS, "sums");
+      float* own = (float*)lds_at<float>(lds) + Place::wave() * (MI * NJ * 1024) + lane;
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+        for (int nj = 0; nj < NJ; ++nj)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) own[Place::wk() * (BI * BJ) + (mi * NJ + nj) * 1024 + r * 64] = acc[mi][nj][r];
+      __syncthreads();
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+        for (int nj = 0; nj < NJ; ++nj)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            float v = own[(mi * NJ + nj) * 1024 + r * 64];
+#pragma unroll
+            for (int w = 1; w < WK; ++w) v += own[w * (BI * BJ) + (mi * NJ + nj) * 1024 + r * 64];
+            acc[mi][nj][r] = v;
+          }
+      __syncthreads();
+    }
   }
 };
 
@@ -257,7 +295,7 @@ struct Tile {
 // STAGED_X: an operand X whose rows are not whole 16-byte units goes through
 // registers instead.
 template <class T, Order OX, Order OY, bool STAGED_X>
-struct BigTile {
+struct BigTile : Waves<2, 2, 1, 4, 4> {
   static constexpr int BI = 256, BJ = 256, BK = 64, WI = 2, WJ = 2, MI = 4, NJ = 4, NT = 256;
   static constexpr uint32_t SLOT = 256 * BK * 2, LDS = 5 * SLOT;
   static constexpr int U = 8;                                     // 16-byte units per thread and operand of a step
@@ -326,8 +364,7 @@ struct BigTile {
 
   static __device__ __forceinline__ void product(const Operand& X, const Operand& Y, int64_t i0, int64_t j0, int64_t k0,
                                                  int64_t kend, uint32_t lds, Acc& acc) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int bi = (wave / WJ) * 128, bj = (wave % WJ) * 128;
+    const int lane = threadIdx.x & 63, bi = Waves<2, 2, 1, 4, 4>::base_i(), bj = Waves<2, 2, 1, 4, 4>::base_j();
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
@@ -540,11 +577,11 @@ __device__ __forceinline__ void write4(float* p, int64_t left, f32x4 v) {
 // A tile of I x J results from its own corner on.
 template <class T, class Tl>
 __device__ __forceinline__ void write_tile(typename Tl::Acc& acc, char* lds, T* out, int64_t ldo, int64_t I, int64_t J) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int bi = (wave / Tl::WJ) * 32 * Tl::MI, bj = (wave % Tl::WJ) * 32 * Tl::NJ;
+  const int lane = threadIdx.x & 63, bi = Tl::base_i(), bj = Tl::base_j();
 #pragma unroll
   for (int nj = 0; nj < Tl::NJ; ++nj) {
     const int j = bj + 32 * nj + (lane & 31);
+    if (!Tl::lead()) break;
 #pragma unroll
     for (int mi = 0; mi < Tl::MI; ++mi)
 #pragma unroll

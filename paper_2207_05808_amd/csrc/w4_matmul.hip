@@ -244,44 +244,45 @@ __global__ void __launch_bounds__(256) w4_quantize_kernel(QArgs a) {
   }
 }
 
-// B with its columns contiguous (stride_m 1): a wavefront takes 64 columns, a
-// lane one of them, so that every load is 128 or 256 bytes of a row and a
-// group's maximum stays in its lane.
+// B with its columns contiguous (stride_m 1): a workgroup takes 64 columns of a
+// block, a lane one of them and a wavefront one group of 32 rows, so that every
+// load is 128 or 256 bytes of a row and a group's maximum stays in its lane; the
+// codes are put together in LDS.
 template <class T>
 __global__ void __launch_bounds__(256) w4_quantize_rows_kernel(QArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15;
+  __shared__ uint32_t words[4][4][64];   // [quarter][group][column]
+  __shared__ uint8_t bytes[64][4];
+  const int lane = threadIdx.x & 63, j = threadIdx.x >> 6;
   const int64_t strips = (a.nm + 3) / 4, blocks = (int64_t)a.nk * strips;
-  for (int64_t b = (int64_t)blockIdx.x * 4 + wave; b < blocks; b += (int64_t)gridDim.x * 4) {
-    const int kb = (int)(b / strips), m = (int)(b % strips) * 64 + lane, mb = m >> 4;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const int kb = (int)(b / strips), m = (int)(b % strips) * 64 + lane, d = kb * kWK + 32 * j;
     const T* src = static_cast<const T*>(a.B) + m;
-    u32x4 word[4];
-    uint32_t exps = 0;
+    float v[4][8], top = 0.0f;
+    bool odd = false;   // not finite
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float v[4][8], top = 0.0f;
-      bool odd = false;
-      const int d = kb * kWK + 32 * j;
+    for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int i = 0; i < 8; ++i) v[q][i] = d + 8 * q + i < a.D && m < a.M ? to_float(src[(d + 8 * q + i) * a.sd]) : 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[q][i] = d + 8 * q + i < a.D && m < a.M ? to_float(src[(d + 8 * q + i) * a.sd]) : 0.0f;
+    for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int i = 0; i < 8; ++i) {
+        top = __builtin_fmaxf(top, __builtin_fabsf(v[q][i]));
+        odd = odd || !(__builtin_fabsf(v[q][i]) < __builtin_inff());
+      }
+    const int e = exponent_of(top, d < a.D && m < a.M);
+    bytes[lane][j] = (uint8_t)(odd ? 255 : e + 127);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          top = __builtin_fmaxf(top, __builtin_fabsf(v[q][i]));
-          odd = odd || !(__builtin_fabsf(v[q][i]) < __builtin_inff());
-        }
-      const int e = exponent_of(top, d < a.D && m < a.M);
-      exps |= (uint32_t)(odd ? 255 : e + 127) << (8 * j);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) word[q][j] = codes_of(v[q], e, odd);
+    for (int q = 0; q < 4; ++q) words[q][j][lane] = codes_of(v[q], e, odd);
+    __syncthreads();
+    // wavefront j writes quarter j of every column
+    const int mb = m >> 4, col = lane & 15;
+    if (mb < a.nm) {
+      const int64_t at = (int64_t)mb * a.nk + kb;
+      reinterpret_cast<u32x4*>(a.codes)[at * 64 + j * 16 + col] = (u32x4){words[j][0][lane], words[j][1][lane], words[j][2][lane], words[j][3][lane]};
+      if (j == 0) reinterpret_cast<uint32_t*>(a.exps)[at * 16 + col] = *reinterpret_cast<const uint32_t*>(bytes[lane]);
     }
-    if (mb >= a.nm) continue;
-    const int64_t at = (int64_t)mb * a.nk + kb;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) reinterpret_cast<u32x4*>(a.codes)[at * 64 + q * 16 + col] = word[q];
-    reinterpret_cast<uint32_t*>(a.exps)[at * 16 + col] = exps;
+    __syncthreads();
   }
 }
 
@@ -290,33 +291,27 @@ struct DArgs {
   void* B;   // [D][M]
 };
 
-// A wavefront takes 64 columns of a block of rows, a lane one of them: every
-// store is 128 or 256 bytes of a row.
+// A workgroup takes 64 columns of a block, a lane one of them, a wavefront one
+// quarter of the rows: every store is 128 or 256 bytes of a row.
 template <class T>
 __global__ void __launch_bounds__(256) w4_dequantize_kernel(DArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15;
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6, col = lane & 15;
   const int64_t strips = (a.nm + 3) / 4, blocks = (int64_t)a.nk * strips;
-  for (int64_t b = (int64_t)blockIdx.x * 4 + wave; b < blocks; b += (int64_t)gridDim.x * 4) {
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
     const int kb = (int)(b / strips), m = (int)(b % strips) * 64 + lane;
     if (m >= a.M) continue;
     const int64_t at = (int64_t)(m >> 4) * a.nk + kb;
     const uint32_t e = reinterpret_cast<const uint32_t*>(a.exps)[at * 16 + col];
-    u32x4 w[4];
+    const u32x4 w = reinterpret_cast<const u32x4*>(a.codes)[at * 64 + q * 16 + col];
+    T* out = static_cast<T*>(a.B) + ((int64_t)kb * kWK + 8 * q) * a.M + m;
+    const int left = a.D - kb * kWK - 8 * q;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) w[q] = reinterpret_cast<const u32x4*>(a.codes)[at * 64 + q * 16 + col];
-    T* out = static_cast<T*>(a.B) + (int64_t)kb * kWK * a.M + m;
-    const int left = a.D - kb * kWK;
+    for (int j = 0; j < 4; ++j) {
+      const bf16x8 v = unpack8(w[j], scale_of(e, j));
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const bf16x8 v = unpack8(w[q][j], scale_of(e, j));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int d = 32 * j + 8 * q + i;
-          if (d < left) out[(int64_t)d * a.M] = from_float<T>((float)v[i]);
-        }
-      }
+      for (int i = 0; i < 8; ++i)
+        if (32 * j + i < left) out[(int64_t)(32 * j + i) * a.M] = from_float<T>((float)v[i]);
+    }
   }
 }
 
@@ -424,13 +419,13 @@ struct WTArgs {
 template <class T, class Y, class Tl>
 __global__ void __launch_bounds__(Tl::NT, 1) w4_tile_kernel(WTArgs a) {
   extern __shared__ __align__(16) char lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
   int64_t it, jt;
   tile_of(blockIdx.x, a.itiles, a.jtiles, it, jt);
   const int64_t i0 = it * Tl::BI, j0 = jt * Tl::BJ;
   typename Tl::Acc acc;
   Tl::product(a.W, a.A, i0, j0, 0, a.K, lds_address(lds), acc);
-  const int bi = (wave / Tl::WJ) * 32 * Tl::MI;
+  const int bi = Tl::base_i();
 #pragma unroll
   for (int mi = 0; mi < Tl::MI; ++mi)
 #pragma unroll
@@ -458,7 +453,7 @@ int blocks_for(int64_t waves, int per) {
 template <class T>
 hipError_t launch_quantize(const QArgs& a, hipStream_t s) {
   const int64_t blocks = (int64_t)a.nk * a.nm;
-  if (a.sm == 1 && a.sd != 1) hipLaunchKernelGGL((w4_quantize_rows_kernel<T>), dim3(blocks_for((int64_t)a.nk * ((a.nm + 3) / 4), 4)), dim3(256), 0, s, a);
+  if (a.sm == 1 && a.sd != 1) hipLaunchKernelGGL((w4_quantize_rows_kernel<T>), dim3(blocks_for((int64_t)a.nk * ((a.nm + 3) / 4), 1)), dim3(256), 0, s, a);
   else if (a.sd == 1) hipLaunchKernelGGL((w4_quantize_kernel<T, true>), dim3(blocks_for(blocks, 4)), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((w4_quantize_kernel<T, false>), dim3(blocks_for(blocks, 4)), dim3(256), 0, s, a);
   return hipGetLastError();
@@ -586,7 +581,7 @@ int maddness_dequantize_w4(const uint8_t* codes, const uint8_t* exps, int32_t D,
   if (dtype != MADDNESS_F32 && dtype != MADDNESS_BF16) return MADDNESS_EINVAL;
   if (!aligned(B_out, dtype == MADDNESS_F32 ? 4 : 2) || !aligned(codes, 16) || !aligned(exps, 4)) return MADDNESS_EINVAL;
   DArgs a{codes, exps, D, M, (int)(((int64_t)D + kWK - 1) / kWK), (int)(((int64_t)M + kWM - 1) / kWM), B_out};
-  const dim3 grid(blocks_for((int64_t)a.nk * ((a.nm + 3) / 4), 4));
+  const dim3 grid(blocks_for((int64_t)a.nk * ((a.nm + 3) / 4), 1));
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (dtype == MADDNESS_F32) hipLaunchKernelGGL((w4_dequantize_kernel<float>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((w4_dequantize_kernel<Bf16>), grid, dim3(256), 0, s, a);
