@@ -83,11 +83,14 @@ __device__ __forceinline__ float w4_sigma(const WArgs& a, float v, int m) {
   return a.act == 2 ? (v > 0.0f ? v : 0.0f) : v;
 }
 
-// One workgroup: 16 columns x 16 RT rows, the wavefronts taking the weight's
-// 128-row blocks in turn and their sums added through LDS.
+// Few rows: one workgroup takes 16 columns x 16 RT rows, the wavefronts the
+// weight's 128-row blocks in turn; their sums are added through LDS.  A
+// wavefront has its next four blocks under way at a time: what bounds a single
+// row is how many bytes are (65536 columns of 4096 rows, one bf16 row: see the
+// figures at launch_w4).
 template <class T, class Y, int RT>
 __global__ void __launch_bounds__(512) w4_rows_kernel(WArgs a) {
-  constexpr int P = Parts<T>::n;
+  constexpr int P = Parts<T>::n, U = 4;
   extern __shared__ float red[];   // [wavefronts][RT][16 rows][16 columns]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int col = lane & 15, quarter = lane >> 4;
@@ -100,20 +103,31 @@ __global__ void __launch_bounds__(512) w4_rows_kernel(WArgs a) {
     f32x4 acc[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) acc[r] = (f32x4){0, 0, 0, 0};
-    for (int kb = wave; kb < a.nk; kb += waves) {
-      const u32x4 w = codes[(int64_t)kb * 64];
-      const uint32_t e = exps[kb * 16];
+    for (int k0 = wave; k0 < a.nk; k0 += waves * U) {
+      u32x4 w[U];
+      uint32_t e[U];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bf16x8 b = unpack8(w[j], scale_of(e, j));
-        const int k = kb * kWK + 32 * j + 8 * quarter;
+      for (int u = 0; u < U; ++u) {
+        const int kb = k0 + u * waves < a.nk ? k0 + u * waves : k0;
+        w[u] = codes[(int64_t)kb * 64];
+        e[u] = exps[kb * 16];
+      }
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          const int64_t n = n0 + 16 * r + col;
-          bf16x8 x[P];
-          load_parts(static_cast<const T*>(a.A) + n * a.lda + k, n < a.N ? a.D - k : 0, x);
+      for (int u = 0; u < U; ++u) {
+        const int kb = k0 + u * waves;
+        if (kb >= a.nk) break;
 #pragma unroll
-          for (int p = P - 1; p >= 0; --p) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[p], b, acc[r], 0, 0, 0);
+        for (int j = 0; j < 4; ++j) {
+          const bf16x8 b = unpack8(w[u][j], scale_of(e[u], j));
+          const int k = kb * kWK + 32 * j + 8 * quarter;
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            const int64_t n = n0 + 16 * r + col < a.N ? n0 + 16 * r + col : a.N - 1;   // (results past the end are not written)
+            bf16x8 x[P];
+            load_parts(static_cast<const T*>(a.A) + n * a.lda + k, a.D - k, x);
+#pragma unroll
+            for (int p = P - 1; p >= 0; --p) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[p], b, acc[r], 0, 0, 0);
+          }
         }
       }
     }
@@ -130,6 +144,138 @@ __global__ void __launch_bounds__(512) w4_rows_kernel(WArgs a) {
       if (n < a.N && m < a.M) static_cast<Y*>(a.y)[n * a.M + m] = from_float<Y>(w4_sigma(a, v, m));
     }
     __syncthreads();
+  }
+}
+
+// More rows: the activations' parts go through LDS, a 128-column block of 16 RT
+// rows at a time (two buffers), and are shared by four wavefronts of 16 CT
+// columns each, whose weights go from memory to registers and are unpacked
+// there, once for all RT row blocks.  KG groups of four wavefronts take the
+// 128-row blocks in turn (each with buffers of its own) where the columns alone
+// do not fill the card; their sums are added through LDS.
+template <class T, class Y, int RT, int CT, int KG>
+__global__ void __launch_bounds__(256 * KG, KG == 1 && Parts<T>::n < 3 ? 2 : 1) w4_block_kernel(WArgs a) {
+  constexpr int P = Parts<T>::n, ROWS = 16 * RT, BUF = P * ROWS * kWK * 2;   // bytes of a buffer
+  constexpr int UNITS = ROWS * 16 / 256;   // 8-column units of a buffer per thread
+  extern __shared__ __align__(16) char lds[];
+  const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
+  const int group = threadIdx.x >> 8, t = threadIdx.x & 255, wave = t >> 6;
+  char* buf = lds + group * (2 * BUF);
+  const int mb0 = (blockIdx.x * 4 + wave) * CT;
+  const int64_t n0 = (int64_t)blockIdx.y * ROWS;
+  // a unit's row and place; rows past the end are read as the last one (their results are not written)
+  auto load_unit = [&](int i, int kb, bf16x8 (&x)[P]) {
+    const int u = t + 256 * i, r = u >> 4, k = kb * kWK + (u & 15) * 8;
+    const int64_t n = n0 + r < a.N ? n0 + r : a.N - 1;
+    load_parts(static_cast<const T*>(a.A) + n * a.lda + k, a.D - k, x);
+  };
+  auto store_unit = [&](int i, char* to, const bf16x8 (&x)[P]) {
+    const int u = t + 256 * i, r = u >> 4, c = u & 15;
+#pragma unroll
+    for (int p = 0; p < P; ++p) *reinterpret_cast<bf16x8*>(to + p * (ROWS * kWK * 2) + r * (kWK * 2) + ((c ^ (r & 15)) << 4)) = x[p];
+  };
+  f32x4 acc[RT][CT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int c = 0; c < CT; ++c) acc[r][c] = (f32x4){0, 0, 0, 0};
+  const u32x4* codes = reinterpret_cast<const u32x4*>(a.codes) + lane;
+  const uint32_t* exps = reinterpret_cast<const uint32_t*>(a.exps) + col;
+  u32x4 w[CT];
+  uint32_t e[CT];
+  auto weights = [&](int kb) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      const int64_t at = (int64_t)(mb0 + c < a.nm ? mb0 + c : a.nm - 1) * a.nk + kb;
+      w[c] = codes[at * 64];
+      e[c] = exps[at * 16];
+    }
+  };
+  const int turns = (a.nk + KG - 1) / KG;   // the same for every group: they meet at the barriers
+  auto block_of = [&](int s) { return s * KG + group < a.nk ? s * KG + group : a.nk - 1; };
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i) {
+    bf16x8 x[P];
+    load_unit(i, block_of(0), x);
+    store_unit(i, buf, x);
+  }
+  weights(block_of(0));
+  for (int s = 0; s < turns; ++s) {
+    char* cur = buf + (s & 1) * BUF;
+    lds_only_barrier();   // this block is in LDS, and everyone is done with the other buffer
+    u32x4 wn[CT];
+    uint32_t en[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) { wn[c] = w[c]; en[c] = e[c]; }
+    const int next = s + 1 < turns ? block_of(s + 1) : block_of(s);
+    weights(next);
+    const bool mine = s * KG + group < a.nk;
+    bf16x8 held[UNITS > 4 ? 4 : UNITS][P];   // the next block's first units, on their way under the products
+#pragma unroll
+    for (int i = 0; i < UNITS && i < 4; ++i) load_unit(i, next, held[i]);
+    if (mine) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bf16x8 b[CT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) b[c] = unpack8(wn[c][j], scale_of(en[c], j));
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          const int row = 16 * r + col;
+#pragma unroll
+          for (int p = P - 1; p >= 0; --p) {
+            const bf16x8 x = *reinterpret_cast<const bf16x8*>(cur + p * (ROWS * kWK * 2) + row * (kWK * 2) + (((4 * j + quarter) ^ (row & 15)) << 4));
+#pragma unroll
+            for (int c = 0; c < CT; ++c) acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, b[c], acc[r][c], 0, 0, 0);
+          }
+        }
+      }
+    }
+    char* to = buf + ((s + 1) & 1) * BUF;
+#pragma unroll
+    for (int i = 0; i < UNITS && i < 4; ++i) store_unit(i, to, held[i]);
+#pragma unroll
+    for (int i = 4; i < UNITS; ++i) {
+      bf16x8 x[P];
+      load_unit(i, next, x);
+      store_unit(i, to, x);
+    }
+  }
+  if constexpr (KG > 1) {
+    float* red = reinterpret_cast<float*>(lds) + t;   // [group][r][c][i][256]
+    __syncthreads();
+    if (group > 0) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) red[(((group - 1) * RT + r) * CT + c) * 1024 + i * 256] = acc[r][c][i];
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int g = 1; g < KG; ++g) acc[r][c][i] += red[(((g - 1) * RT + r) * CT + c) * 1024 + i * 256];
+  }
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int m = (mb0 + c) * kWM + col;
+    if (m >= a.M) continue;
+    const float bias = a.bias ? a.bias[m] : 0.0f;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t n = n0 + 16 * r + 4 * quarter + i;
+        const float v = acc[r][c][i] + bias;
+        if (n < a.N) static_cast<Y*>(a.y)[n * a.M + m] = from_float<Y>(a.act == 2 && !(v > 0.0f) ? 0.0f : v);
+      }
   }
 }
 
@@ -468,8 +614,32 @@ hipError_t launch_rows(const WArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// From how many rows on the weights are unpacked first.
-constexpr int64_t kManyRows = 128;
+template <class T, class Y, int RT, int CT, int KG>
+hipError_t launch_block(WArgs a, hipStream_t stream) {
+  constexpr int kBuffers = KG * 2 * Parts<T>::n * 16 * RT * kWK * 2, kSums = (KG - 1) * RT * CT * 4096;
+  constexpr int kLds = kBuffers > kSums ? kBuffers : kSums;
+  static_assert(kLds <= kLdsBytes, "LDS");
+  hipError_t err = hipSuccess;
+  auto kernel = w4_block_kernel<T, Y, RT, CT, KG>;
+  launch_prepare(reinterpret_cast<const void*>(kernel), 256 * KG, kLds, &err);
+  if (err != hipSuccess) return err;
+  constexpr int64_t kRows = 65535ll * 16 * RT;   // of one launch
+  for (int64_t left = a.N; left > 0; left -= kRows) {
+    a.N = left < kRows ? left : kRows;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv(a.nm, 4 * CT), (unsigned)cdiv(a.N, 16 * RT)), dim3(256 * KG), kLds, stream, a);
+    if ((err = hipGetLastError()) != hipSuccess) return err;
+    a.A = static_cast<const T*>(a.A) + kRows * a.lda;
+    a.y = static_cast<Y*>(a.y) + kRows * a.M;
+  }
+  return hipSuccess;
+}
+
+// From how many rows on the weights are unpacked first, which costs about 1.2
+// ps a weight.  The block kernel then multiplies at 0.9 PFLOP/s a part of the
+// activations (bf16 one, fp16 two, fp32 three) and the tiles at 1.2 to 1.3 (fp16
+// one part): 4096 -> 65536, 512 rows of bf16 303 against 383 us, of fp32 827
+// against 748.
+constexpr int64_t many_rows(int32_t dtype) { return dtype == MADDNESS_BF16 ? 1536 : dtype == MADDNESS_F16 ? 448 : 1024; }
 
 // The plan for many rows; bytes: workspace, 0 where the rows kernel takes the call.
 struct Many {
@@ -478,7 +648,7 @@ struct Many {
 };
 Many plan_many(const void* A, int32_t dtype, int64_t N, int32_t D, int64_t lda, int32_t M) {
   Many p{};
-  if (N <= kManyRows) return p;
+  if (N <= many_rows(dtype)) return p;
   p.parts = dtype == MADDNESS_F32 ? 3 : 1;
   p.direct = dtype != MADDNESS_F32 && D % 64 == 0 && direct(Operand{A, lda, N, N, 0}, false);
   p.per = ((int64_t)D + kWK - 1) / kWK * kWK;
@@ -543,9 +713,17 @@ template <class T, class Y>
 hipError_t launch_w4(const WArgs& a, const Many& p, char* ws, hipStream_t stream) {
   if (p.bytes > 0 && ws)
     return launch_many<T, typename std::conditional<std::is_same<T, F16>::value, F16, Bf16>::type, Y>(a, p, ws, stream);
-  if (a.N <= 16) return launch_rows<T, Y, 1>(a, stream);
-  if (a.N <= 32) return launch_rows<T, Y, 2>(a, stream);
-  return launch_rows<T, Y, 4>(a, stream);
+  // (9 to 16 rows of a wide layer too: 4096 -> 65536, 16 of bf16 52 against 74 us)
+  if (a.N <= 8 || (a.N <= 16 && cdiv(a.nm, 16) < 160)) return launch_rows<T, Y, 1>(a, stream);
+  // more rows: the widest wavefronts that still leave a workgroup for most compute units
+  const int64_t rows = cdiv(a.N, 64);
+  if (cdiv(a.nm, 16) * rows >= 160) return launch_block<T, Y, 4, 4, 1>(a, stream);
+  if (cdiv(a.nm, 8) * rows >= 160) return launch_block<T, Y, 4, 2, 1>(a, stream);
+  if (cdiv(a.nm, 4) * rows >= 160 || a.nk == 1) return launch_block<T, Y, 4, 1, 1>(a, stream);
+  // (as many groups as have LDS for their buffers)
+  if constexpr (Parts<T>::n == 1) return launch_block<T, Y, 4, 1, 4>(a, stream);
+  else if constexpr (Parts<T>::n == 2) return launch_block<T, Y, 2, 1, 4>(a, stream);
+  else return launch_block<T, Y, 2, 1, 3>(a, stream);
 }
 
 }  // namespace

@@ -56,9 +56,9 @@ def test_matmul_rejects(L):
         (10, NULL, 1), (11, 2, 1), (0, at(1), 1), (5, at(8), 1), (6, at(2), 1), (8, at(2), 1), (10, at(1), 1)])
     rejects(L.maddness_matmul_w4, good, [(9, 3, 1)])   # a softmax in 16 bits
     assert L.maddness_matmul_w4(NULL, 1, 0, 64, 64, NULL, NULL, 16, NULL, 0, NULL, 1, NULL, 0, NULL) == 0
-    size = L.maddness_matmul_w4_workspace_bytes(FAKE, 1, 1000, 64, 64, 512)
+    size = L.maddness_matmul_w4_workspace_bytes(FAKE, 1, 4000, 64, 64, 512)
     assert size > 0
-    many = [FAKE, 1, 1000, 64, 64, FAKE, FAKE, 512, NULL, 0, FAKE, 1, FAKE, size, NULL]
+    many = [FAKE, 1, 4000, 64, 64, FAKE, FAKE, 512, NULL, 0, FAKE, 1, FAKE, size, NULL]
     rejects(L.maddness_matmul_w4, many, [(12, at(64), 1), (13, size - 1, 1), (13, 0, 1)])
     Q = L.maddness_matmul_w4_workspace_bytes
     assert Q(FAKE, 1, 1, 64, 64, 512) == 0 and Q(NULL, 0, 0, 64, 64, 512) == 0

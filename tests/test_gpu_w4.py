@@ -133,7 +133,7 @@ def check(A, w, bias, act, out_dtype=None):
     return y
 
 
-@pytest.mark.parametrize("N", [1, 2, 15, 16, 17, 33, 64, 65, 200, 513])
+@pytest.mark.parametrize("N", [1, 2, 15, 16, 17, 33, 64, 65, 200, 513, 1537])
 @pytest.mark.parametrize("D,M", [(1, 1), (64, 10), (127, 31), (512, 100), (1000, 257), (4100, 48)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
 def test_matmul(N, D, M, dtype):
@@ -141,7 +141,7 @@ def test_matmul(N, D, M, dtype):
     check(rand((N, D), 4, dtype), w, None, "none")
 
 
-@pytest.mark.parametrize("N,D,M", [(2500, 128, 5000), (3000, 321, 4099), (257, 64, 50003)])
+@pytest.mark.parametrize("N,D,M", [(2500, 128, 5000), (3000, 321, 4099), (1600, 64, 30003)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
 def test_many_rows(N, D, M, dtype):
     """More tiles than compute units; with the caller's workspace (dirty) and
@@ -170,17 +170,17 @@ def test_exponents_far_apart(dtype):
     B[:, 11] *= 2.0 ** -80
     B[:, 12] = 0.0
     w = mdn.quantize_w4(B)
-    A = rand((300, D), 4, dtype)
+    A = rand((1700, D), 4, dtype)
     A[:, :32] = 0
     A[:, 64:] = 0     # only the small groups are left
     W = mdn.dequantize_w4(w, dtype=torch.float32).double()
-    for rows in (A, A[:9]):
+    for rows in (A, A[:300], A[:9]):
         y = mdn.matmul_w4(rows, w, out_dtype=torch.float32).double()
         ref, size = rows.double() @ W, rows.double().abs() @ W.abs()
         assert bool(((y - ref).abs() <= size * 70 * 2.0 ** -23).all())
 
 
-@pytest.mark.parametrize("N,D,M", [(1, 256, 130), (5, 300, 7), (70, 129, 1003), (300, 512, 512)])
+@pytest.mark.parametrize("N,D,M", [(1, 256, 130), (5, 300, 7), (70, 129, 1003), (300, 512, 512), (40, 700, 9000), (100, 200, 20000), (130, 257, 45000)])
 @pytest.mark.parametrize("act", ["bias", "relu", "softmax"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_layer_output(N, D, M, act, dtype):
@@ -234,7 +234,7 @@ def test_values_that_are_not_finite(dtype):
     B[7, 9] = 0.0
     w = mdn.quantize_w4(B)
     W = mdn.dequantize_w4(w, dtype=torch.float32)
-    for N in (4, 90, 300):
+    for N in (4, 90, 600, 1700):
         A = rand((N, D), 4, dtype)
         A[1, 7] = math.inf
         A[2, 100] = math.nan
@@ -247,7 +247,7 @@ def test_values_that_are_not_finite(dtype):
     half = mdn.quantize_w4(torch.full((D, 1), 2.0 ** -20, device=DEV))
     check(big, half, None, "none", torch.float32)
     B[150, 3] = math.nan
-    for N in (4, 300):
+    for N in (4, 300, 1700):
         y = mdn.matmul_w4(rand((N, D), 4, dtype), mdn.quantize_w4(B))
         assert y[:, 3].isnan().all() and torch.isfinite(y[:, 4:]).all()
 
