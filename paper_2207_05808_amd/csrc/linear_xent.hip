@@ -28,6 +28,7 @@ struct XArgs {
   const int64_t* target;    // [N]
   float2* part;             // [N][tiles]: a tile's maximum and sum
   float* zt;                // [N]: the target's logit
+  float* loss; float* lse_out;   // [N] (forward)
   int64_t m0, m1;           // outputs of this piece (gradient)
   const float* lse; const float* gloss;
   void* dz; int64_t ldz;    // [N][ldz]: the piece's G
@@ -39,6 +40,15 @@ struct XArgs {
 __device__ __forceinline__ int target_at(int64_t t, int64_t M, int64_t i0) {
   const int64_t d = t - i0;
   return t < 0 || t >= M || d < 0 || d >= (1 << 20) ? -1 : (int)d;
+}
+
+// a row's lse and loss from its maximum, its sum and its target's logit (looked
+// at where there is one)
+__device__ __forceinline__ void finish(const XArgs& a, int64_t n, float top, float sum, float z) {
+  const float l = top + logf(sum);
+  const int64_t t = a.target[n];
+  a.lse_out[n] = l;
+  a.loss[n] = t < 0 || t >= a.M ? 0.0f : l == -__builtin_inff() ? __builtin_inff() : l - z;
 }
 
 template <class T, class Tl>
@@ -55,6 +65,7 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
   float b[Tl::MI][16];
   load_bias<Tl>(b, a.bias, i0 + bi, a.M);
   float2* red = reinterpret_cast<float2*>(lds);   // [WI][BJ]
+  float* zl = reinterpret_cast<float*>(red + WI * BJ);   // [BJ]: targets' logits, where this is a row's only tile
 #pragma unroll
   for (int nj = 0; nj < Tl::NJ; ++nj) {
     const int64_t j = j0 + bj + 32 * nj + (lane & 31);
@@ -68,7 +79,7 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
         asm volatile("");   // (a branch: seldom taken)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (t == 32 * mi + entry_row(r, lane)) a.zt[j] = acc[mi][nj][r] + b[mi][r];
+          if (t == 32 * mi + entry_row(r, lane)) (a.itiles == 1 ? zl : a.zt + j0)[j - j0] = acc[mi][nj][r] + b[mi][r];
       }
     }
     top = __builtin_fmaxf(top, __shfl_xor(top, 32));
@@ -91,30 +102,26 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
       const float top = __builtin_fmaxf(v.x, u.x), b = base_of(top);
       v = make_float2(top, v.y * exp_of(v.x - b) + u.y * exp_of(u.x - b));
     }
-    a.part[(j0 + j) * a.itiles + it] = v;
+    if (a.itiles == 1) finish(a, j0 + j, v.x, v.y, zl[j]);
+    else a.part[(j0 + j) * a.itiles + it] = v;
   }
 }
 
 // One wavefront per row: lse and loss from the row's tiles.
-__global__ void __launch_bounds__(256) xent_join_kernel(const float2* part, const float* zt, const int64_t* target, int64_t N,
-                                                        int64_t M, int64_t tiles, float* loss, float* lse) {
+__global__ void __launch_bounds__(256) xent_join_kernel(XArgs a) {
   const int lane = threadIdx.x & 63;
-  for (int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); n < N; n += (int64_t)gridDim.x * 4) {
+  for (int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); n < a.N; n += (int64_t)gridDim.x * 4) {
+    const float2* part = a.part + n * a.itiles;
     float top = -__builtin_inff();
-    for (int64_t t = lane; t < tiles; t += 64) top = __builtin_fmaxf(top, part[n * tiles + t].x);
+    for (int64_t t = lane; t < a.itiles; t += 64) top = __builtin_fmaxf(top, part[t].x);
     for (int o = 1; o < 64; o <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
     float sum = 0.0f;
-    for (int64_t t = lane; t < tiles; t += 64) {
-      const float2 v = part[n * tiles + t];
+    for (int64_t t = lane; t < a.itiles; t += 64) {
+      const float2 v = part[t];
       sum += v.y * exp_of(v.x - base_of(top));
     }
     for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    if (lane == 0) {
-      const float l = top + logf(sum);
-      const int64_t t = target[n];
-      lse[n] = l;
-      loss[n] = t < 0 || t >= M ? 0.0f : l == -__builtin_inff() ? __builtin_inff() : l - zt[n];
-    }
+    if (lane == 0) finish(a, n, top, sum, a.zt[n]);
   }
 }
 
@@ -346,7 +353,7 @@ template <class T>
 int row_tile(const XArgs& a, int64_t outputs) {
   if (sizeof(T) == 2 && a.N >= 192 && direct(a.A, false) && cdiv(a.N, 256) * cdiv(outputs, 256) >= 192) return 256;
   if (a.N > 64 && cdiv(a.N, 128) * cdiv(outputs, 128) >= 256) return 128;
-  return a.N > 32 && cdiv(a.N, 64) * cdiv(outputs, 128) >= 256 ? 64 : 32;
+  return a.N > 32 && cdiv(a.N, 32) * cdiv(outputs, 128) > 256 ? 64 : 32;
 }
 
 template <class T, bool GRAD>
@@ -361,8 +368,19 @@ hipError_t logits(XArgs& a, int64_t outputs, int rows, bool md, hipStream_t s) {
   }
   if (rows >= 128) return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>>(a, outputs, s)
                              : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 128, 2, 2>>(a, outputs, s);
-  if (rows == 64) return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 64, 4, 1>>(a, outputs, s)
-                            : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 64, 4, 1>>(a, outputs, s);
+  // Where every workgroup has a compute unit to itself: twice the wavefronts,
+  // each for half of the k of a step twice as long, since one wavefront to a SIMD
+  // waits for the stages of a step in turn.
+  const bool alone = cdiv(a.N, rows) * cdiv(outputs, 128) <= 256;
+  constexpr int BK = sizeof(T) == 2 ? 64 : 32;
+  if (rows == 64) {
+    if (alone) return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 64, 4, 1, 2 * BK, 2>>(a, outputs, s)
+                         : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 64, 4, 1, 2 * BK, 2>>(a, outputs, s);
+    return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 64, 4, 1>>(a, outputs, s)
+              : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 64, 4, 1>>(a, outputs, s);
+  }
+  if (alone) return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 32, 4, 1, 2 * BK, 2>>(a, outputs, s)
+                       : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 32, 4, 1, 2 * BK, 2>>(a, outputs, s);
   return md ? launch_logits<T, GRAD, Tile<T, kAlongK, kAlongK, 128, 32, 4, 1>>(a, outputs, s)
             : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 32, 4, 1>>(a, outputs, s);
 }
@@ -483,11 +501,12 @@ hipError_t grad(XArgs a, bool md, void* dA, void* dB, float* dbias, char* ws, hi
 
 template <class T>
 hipError_t forward(XArgs a, bool md, float* loss, float* lse, hipStream_t s) {
+  a.loss = loss;
+  a.lse_out = lse;
   hipError_t e = logits<T, false>(a, a.M, row_tile<T>(a, a.M), md, s);
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.itiles == 1) return e;
   const int64_t b = cdiv(a.N, 4);
-  hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)(b < 65536 ? b : 65536)), dim3(256), 0, s, a.part, a.zt, a.target, a.N, a.M,
-                     a.itiles, loss, lse);
+  hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)(b < 65536 ? b : 65536)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

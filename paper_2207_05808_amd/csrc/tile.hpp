@@ -74,7 +74,7 @@ struct Tile : Waves<WI_, WJ_, WK, BI_ / WI_ / 32, BJ_ / WJ_ / 32> {
   static __device__ __forceinline__ int at(int r, int k) {
     if constexpr (O == kAlongK) {
       constexpr int U = BK / 8;
-      const int s = U == 8 ? (r >> 1) & 7 : (r >> 2) & 3;
+      const int s = U == 16 ? r & 15 : U == 8 ? (r >> 1) & 7 : (r >> 2) & 3;
       return r * (BK * 2) + (((k >> 3) ^ s) << 4) + (k & 7) * 2;
     } else {
       constexpr int NB = B / 32;
