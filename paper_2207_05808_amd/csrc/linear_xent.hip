@@ -469,13 +469,15 @@ hipError_t grad(XArgs a, bool md, void* dA, void* dB, float* dbias, char* ws, hi
     x.first = m0 == 0; x.last = m0 + n == a.M;
     bool done = false;
     if constexpr (sizeof(T) == 2) {
-      if (a.N >= 256 && a.D >= 256) {
+      // (as many tiles and shares of at least 1024 outputs as most compute units)
+      if (a.N >= 192 && a.D >= 192 && cdiv(a.N, 256) * cdiv(a.D, 256) * cdiv(n, 1024) >= 192) {
         done = true;
         if (direct(x.X, md)) e = md ? gemm<T, BigTile<T, kAlongI, kAlongK, false>, true>(x, g.part, s) : gemm<T, BigTile<T, kAlongK, kAlongK, false>, true>(x, g.part, s);
         else e = md ? gemm<T, BigTile<T, kAlongI, kAlongK, true>, true>(x, g.part, s) : gemm<T, BigTile<T, kAlongK, kAlongK, true>, true>(x, g.part, s);
       }
     }
     if (done) {}
+    else if (cdiv(a.N, 128) * cdiv(a.D, 128) < 512) e = md ? gemm<T, Tile<T, kAlongI, kAlongK, 128, 64, 2, 2>, true>(x, g.part, s) : gemm<T, Tile<T, kAlongK, kAlongK, 128, 64, 2, 2>, true>(x, g.part, s);
     else if (a.N <= 32) e = md ? gemm<T, Tile<T, kAlongI, kAlongK, 128, 32, 4, 1>, true>(x, g.part, s) : gemm<T, Tile<T, kAlongK, kAlongK, 128, 32, 4, 1>, true>(x, g.part, s);
     else e = md ? gemm<T, Tile<T, kAlongI, kAlongK, 128, 128, 2, 2>, true>(x, g.part, s) : gemm<T, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>, true>(x, g.part, s);
     if (e != hipSuccess) return e;

@@ -62,7 +62,9 @@ struct Tile : Waves<WI_, WJ_, WK, BI_ / WI_ / 32, BJ_ / WJ_ / 32> {
   static constexpr int XB = BI * BK * 2, YB = BJ * BK * 2;               // bytes of one part's LDS tile
   static constexpr int STAGE = P * (XB + YB);
   static constexpr int LDS = 2 * STAGE;
-  static constexpr int AHEAD = 3;   // steps loaded ahead into registers: memory takes longer than a step's products
+  // steps loaded ahead into registers: memory takes longer than a step's products
+  // (of 16-bit types; fp32's splits and six products take longer than it)
+  static constexpr int AHEAD = P == 1 ? 3 : 1;
   static_assert(XU * CH * NT == BI * BK && YU * CH * NT == BJ * BK && MI * WI * 32 == BI && NJ * WJ * 32 == BJ, "tile");
   typedef f32x16 Acc[MI][NJ];
 
@@ -120,28 +122,35 @@ struct Tile : Waves<WI_, WJ_, WK, BI_ / WI_ / 32, BJ_ / WJ_ / 32> {
     }
   }
 
-  // units of any step, zeros past the matrix and past kend
+  // units of any step, zeros past the matrix and past kend: those inside first,
+  // so that all of them are under way at once, then those that the end cuts
   template <Order O, int B, int U>
   static __device__ __forceinline__ void load(const Operand& o, int64_t r0, int64_t k0, int64_t kend, u32x4 (&v)[U]) {
     const T* base = static_cast<const T*>(o.p) + (O == kAlongK ? r0 * o.ld + k0 : k0 * o.ld + r0);
+    bool cut = false;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       int r, k;
       unit<O, B>(threadIdx.x + i * NT, r, k);
-      const T* p = base + (O == kAlongK ? r * o.ld + k : k * o.ld + r);
-      // elements of the unit inside the matrix
-      const bool in = r0 + r < o.rows && k0 + k < kend;
-      const int64_t left = !in ? 0 : O == kAlongK ? kend - (k0 + k) : o.rows - (r0 + r);
+      const int64_t left = r0 + r >= o.rows || k0 + k >= kend ? 0 : O == kAlongK ? kend - (k0 + k) : o.rows - (r0 + r);
       v[i] = (u32x4){0, 0, 0, 0};
-      if (left >= CH) {
-        v[i] = load16(p);
-      } else if (left > 0) {
+      if (left >= CH) v[i] = load16(base + (O == kAlongK ? r * o.ld + k : k * o.ld + r));
+      cut |= left > 0 && left < CH;
+    }
+    if (__any(cut)) {
 #pragma unroll
-        for (int e = 0; e < CH; ++e)
-          if (e < left) {
-            if constexpr (CH == 4) v[i][e] = __float_as_uint(p[e]);
-            else v[i][e >> 1] |= (uint32_t)p[e].bits << (16 * (e & 1));
-          }
+      for (int i = 0; i < U; ++i) {
+        int r, k;
+        unit<O, B>(threadIdx.x + i * NT, r, k);
+        const int64_t left = r0 + r >= o.rows || k0 + k >= kend ? 0 : O == kAlongK ? kend - (k0 + k) : o.rows - (r0 + r);
+        if (left <= 0 || left >= CH) continue;
+        const T* p = base + (O == kAlongK ? r * o.ld + k : k * o.ld + r);
+#pragma unroll
+        for (int e = 0; e < CH - 1; ++e) {
+          const T x = p[e < left ? e : 0];
+          if constexpr (CH == 4) v[i][e] = e < left ? __float_as_uint(x) : 0u;
+          else v[i][e >> 1] |= (e < left ? (uint32_t)x.bits : 0u) << (16 * (e & 1));
+        }
       }
     }
   }
