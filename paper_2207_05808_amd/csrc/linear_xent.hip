@@ -65,11 +65,11 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
   float b[Tl::MI][16];
   load_bias<Tl>(b, a.bias, i0 + bi, a.M);
   float2* red = reinterpret_cast<float2*>(lds);   // [WI][BJ]
-  float* zl = reinterpret_cast<float*>(red + WI * BJ);   // [BJ]: targets' logits, where this is a row's only tile
+  float* zl = reinterpret_cast<float*>(red + WI * BJ);   // [BJ]: targets' logits, and a place for what is none
 #pragma unroll
   for (int nj = 0; nj < Tl::NJ; ++nj) {
     const int64_t j = j0 + bj + 32 * nj + (lane & 31);
-    const int t = j < a.N && Tl::lead() ? target_at(a.target[j], a.M, i0 + bi) : -1;
+    const int t = target_at(a.target[j < a.N ? j : a.N - 1], a.M, i0 + bi);
     float top = -__builtin_inff();
 #pragma unroll
     for (int mi = 0; mi < Tl::MI; ++mi) {
@@ -77,9 +77,15 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
       for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, acc[mi][nj][r] + b[mi][r]);
       if (__any(t >= 32 * mi && t < 32 * mi + 32)) {
         asm volatile("");   // (a branch: seldom taken)
+        float z = 0.0f;
+        bool mine = false;
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (t == 32 * mi + entry_row(r, lane)) (a.itiles == 1 ? zl : a.zt + j0)[j - j0] = acc[mi][nj][r] + b[mi][r];
+        for (int r = 0; r < 16; ++r) {
+          const bool here = t == 32 * mi + entry_row(r, lane);
+          z = here ? acc[mi][nj][r] + b[mi][r] : z;
+          mine = mine || here;
+        }
+        zl[mine ? bj + 32 * nj + (lane & 31) : BJ] = z;
       }
     }
     top = __builtin_fmaxf(top, __shfl_xor(top, 32));
@@ -90,7 +96,7 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) sum += exp_of(acc[mi][nj][r] + b[mi][r] - base);
     sum += __shfl_xor(sum, 32);
-    if (lane < 32 && Tl::lead()) red[Tl::wi() * BJ + bj + 32 * nj + lane] = make_float2(top, sum);
+    red[Tl::wi() * BJ + bj + 32 * nj + (lane & 31)] = make_float2(top, sum);   // (the same from both halves)
   }
   __syncthreads();
   for (int j = threadIdx.x; j < BJ; j += Tl::NT) {
@@ -102,8 +108,13 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_tile_kernel(XArgs a) {
       const float top = __builtin_fmaxf(v.x, u.x), b = base_of(top);
       v = make_float2(top, v.y * exp_of(v.x - b) + u.y * exp_of(u.x - b));
     }
-    if (a.itiles == 1) finish(a, j0 + j, v.x, v.y, zl[j]);
-    else a.part[(j0 + j) * a.itiles + it] = v;
+    if (a.itiles == 1) {
+      finish(a, j0 + j, v.x, v.y, zl[j]);
+    } else {
+      a.part[(j0 + j) * a.itiles + it] = v;
+      const int t = target_at(a.target[j0 + j], a.M, i0);
+      if (t >= 0 && t < BI) a.zt[j0 + j] = zl[j];
+    }
   }
 }
 
@@ -122,37 +133,6 @@ __global__ void __launch_bounds__(256) xent_join_kernel(XArgs a) {
     }
     for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
     if (lane == 0) finish(a, n, top, sum, a.zt[n]);
-  }
-}
-
-// Adds what a tile of 32-bit sums (as write_tile writes them) holds.
-template <class Tl>
-__device__ __forceinline__ void add_tile(typename Tl::Acc& acc, const float* sum, int64_t ld, int64_t I, int64_t J) {
-  const int lane = threadIdx.x & 63, bi = Tl::base_i(), bj = Tl::base_j();
-#pragma unroll
-  for (int nj = 0; nj < Tl::NJ; ++nj) {
-    const int j = bj + 32 * nj + (lane & 31);
-#pragma unroll
-    for (int mi = 0; mi < Tl::MI; ++mi) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int i = bi + 32 * mi + 8 * q + 4 * (lane >> 5);
-        const float* p = sum + j * ld + i;
-        f32x4 v = {0, 0, 0, 0};
-        if (j < J) {
-          if (i + 4 <= I) {
-            v = __builtin_bit_cast(f32x4, load16(p));
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (i + e < I) v[e] = p[e];
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[mi][nj][4 * q + e] += v[e];
-      }
-      __builtin_amdgcn_sched_barrier(0);   // (a few loads at a time: few registers)
-    }
   }
 }
 
@@ -192,10 +172,9 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_dz_kernel(XArgs a) {
 #pragma unroll
   for (int nj = 0; nj < Tl::NJ; ++nj) {
     const int64_t j = j0 + bj + 32 * nj + (lane & 31);
-    const int64_t target = j < a.N ? a.target[j] : -1;
-    const float l = j < a.N ? a.lse[j] : 0.0f;
-    const bool live = target >= 0 && target < a.M && l != -__builtin_inff();
-    const float g = live ? a.gloss[j] : 0.0f;
+    const int64_t at = j < a.N ? j : a.N - 1, target = a.target[at];   // (rows past the end are not written)
+    const float l = a.lse[at], g = a.gloss[at];
+    const bool live = j < a.N && target >= 0 && target < a.M && l != -__builtin_inff();
     const int t = live ? target_at(target, a.M, i0 + bi) : -1;
 #pragma unroll
     for (int mi = 0; mi < Tl::MI; ++mi) {
@@ -206,7 +185,7 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_dz_kernel(XArgs a) {
         asm volatile("");   // (a branch: seldom taken)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (t == 32 * mi + entry_row(r, lane)) v[r] -= 1.0f;
+          v[r] -= t == 32 * mi + entry_row(r, lane) ? 1.0f : 0.0f;
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -301,9 +280,11 @@ __global__ void __launch_bounds__(Tl::NT, 1) xent_gemm_kernel(GemmArgs a) {
   typename Tl::Acc acc;
   Tl::product(a.X, a.Y, i0, j0, k0, kend, lds_address(lds), acc);
   float* sum = (a.splits > 1 ? a.part + blockIdx.y * I * J : a.sum) + j0 * I + i0;
-  if constexpr (MODE == kMore || MODE == kLast) add_tile<Tl>(acc, sum, I, I - i0, J - j0);
-  if constexpr (MODE == kOut || MODE == kLast) write_tile<T, Tl>(acc, lds, static_cast<T*>(a.out) + j0 * a.ldo + i0, a.ldo, I - i0, J - j0);
-  else write_tile<float, Tl>(acc, lds, sum, I, I - i0, J - j0);
+  T* out = static_cast<T*>(a.out) + j0 * a.ldo + i0;
+  if constexpr (MODE == kOut) write_tile<T, Tl>(acc, lds, out, a.ldo, I - i0, J - j0);
+  else if constexpr (MODE == kPart) write_tile32<float, Tl, false>(acc, lds, sum, I, I - i0, J - j0);
+  else if constexpr (MODE == kMore) write_tile32<float, Tl, true>(acc, lds, sum, I, I - i0, J - j0, sum, I);
+  else write_tile32<T, Tl, true>(acc, lds, out, a.ldo, I - i0, J - j0, sum, I);
 }
 
 // Joins the shares of a split product, in order.

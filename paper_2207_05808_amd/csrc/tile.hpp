@@ -155,6 +155,44 @@ struct Tile : Waves<WI_, WJ_, WK, BI_ / WI_ / 32, BJ_ / WJ_ / 32> {
     }
   }
 
+  // The same without a divergent branch (for BigTile, whose sums leave no
+  // registers to save around one; its operands have 8 elements and more): units
+  // inside are loaded as they are and the others' places from the operand's
+  // start, then, where an end cuts units, every element from the nearest one.
+  template <Order O, int B, int U>
+  static __device__ __forceinline__ void load_flat(const Operand& o, int64_t r0, int64_t k0, int64_t kend, u32x4 (&v)[U]) {
+    const T *origin = static_cast<const T*>(o.p), *base = origin + (O == kAlongK ? r0 * o.ld + k0 : k0 * o.ld + r0);
+    const int64_t last_r = o.rows - 1 - r0, last_k = kend - 1 - k0;
+    const bool cuts = (O == kAlongK ? kend - k0 : o.rows - r0) % CH != 0;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      int r, k;
+      unit<O, B>(threadIdx.x + i * NT, r, k);
+      const bool full = O == kAlongK ? r <= last_r && k + CH - 1 <= last_k : r + CH - 1 <= last_r && k <= last_k;
+      v[i] = load16(full ? base + (O == kAlongK ? r * o.ld + k : k * o.ld + r) : origin);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i][e] = full ? v[i][e] : 0u;
+    }
+    if (cuts) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        int r, k;
+        unit<O, B>(threadIdx.x + i * NT, r, k);
+        const bool cut = O == kAlongK ? r <= last_r && k <= last_k && k + CH - 1 > last_k : r <= last_r && r + CH - 1 > last_r && k <= last_k;
+#pragma unroll
+        for (int e = 0; e < CH - 1; ++e) {
+          const int re = O == kAlongK ? r : r + e, ke = O == kAlongK ? k + e : k;
+          const int64_t rc = re < last_r ? re : last_r, kc = ke < last_k ? ke : last_k;
+          const T x = base[O == kAlongK ? rc * o.ld + kc : kc * o.ld + rc];
+          const bool in = cut && re <= last_r && ke <= last_k;
+          if constexpr (CH == 4) v[i][e] = in ? __float_as_uint(x) : v[i][e];
+          else v[i][e >> 1] |= (in ? (uint32_t)x.bits : 0u) << (16 * (e & 1));
+        }
+        __builtin_amdgcn_sched_barrier(0);   // (a unit at a time: few registers)
+      }
+    }
+  }
+
   template <Order O, int B, int U>
   static __device__ __forceinline__ void store(uint32_t lds, const u32x4 (&v)[U]) {
 #pragma unroll
@@ -333,10 +371,11 @@ struct BigTile : Waves<2, 2, 1, 4, 4> {
 
   // 16 bytes a lane from base + off to LDS, 1 KB from `to` on (uniform).  In
   // assembly, since the compiler has every LDS read wait for all transfers under
-  // way that it knows of; product() waits for those that a read needs.
+  // way that it knows of; product() waits for those that a read needs.  (The
+  // wait states cover a base that a vector instruction has just written, too.)
   static __device__ __forceinline__ void transfer(const char* base, uint32_t off, uint32_t to) {
 #ifdef __OPTIMIZE__
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
 #else   // (uniform values stay in vector registers there, which the assembly cannot take)
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base + off), lds_at<void>(to), 16, 0, 0);
 #endif
@@ -390,7 +429,7 @@ struct BigTile : Waves<2, 2, 1, 4, 4> {
     auto fetch = [&](int s) {   // a staged step to registers
       if constexpr (STAGED_X) {
         if (s < whole_x) Small::template load_whole<OX, 256, U>(X, i0, k0 + (int64_t)s * BK, held);
-        else Small::template load<OX, 256, U>(X, i0, k0 + (int64_t)s * BK, kend, held);
+        else Small::template load_flat<OX, 256, U>(X, i0, k0 + (int64_t)s * BK, kend, held);
       }
     };
     auto put = [&](uint32_t at) {   // and from there to its slot
@@ -470,9 +509,9 @@ struct BigTile : Waves<2, 2, 1, 4, 4> {
     }
     if (k0 + (int64_t)steps * BK < kend) {   // the last, partial step
       u32x4 v[U];
-      Small::template load<OX, 256, U>(X, i0, k0 + (int64_t)steps * BK, kend, v);
+      Small::template load_flat<OX, 256, U>(X, i0, k0 + (int64_t)steps * BK, kend, v);
       Small::template store<OX, 256, U>(lds, v);
-      Small::template load<OY, 256, U>(Y, j0, k0 + (int64_t)steps * BK, kend, v);
+      Small::template load_flat<OY, 256, U>(Y, j0, k0 + (int64_t)steps * BK, kend, v);
       Small::template store<OY, 256, U>(lds + SLOT, v);
       __syncthreads();
       for (int ks = 0; ks < 4; ++ks) {
@@ -505,22 +544,27 @@ __device__ __forceinline__ void tile_of(uint32_t block, int64_t itiles, int64_t 
 __device__ __forceinline__ int entry_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 
 // What is added to a wavefront's products, whose outputs begin at i0: the bias
-// of each, -inf past the last output.
+// of each, -inf past the last output.  (No divergent branch while the sums fill
+// the registers: see load_flat.)
 template <class Tl>
 __device__ __forceinline__ void load_bias(float (&b)[Tl::MI][16], const float* bias, int64_t i0, int64_t M) {
   const int lane = threadIdx.x & 63;
+  const bool inside = i0 + 32 * Tl::MI <= M;   // (uniform)
 #pragma unroll
   for (int mi = 0; mi < Tl::MI; ++mi)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int64_t i = i0 + 32 * mi + entry_row(4 * q, lane);
-      if (i + 4 <= M) {
+      if (inside) {
         const f32x4 v = bias ? __builtin_bit_cast(f32x4, load16(bias + i)) : (f32x4){0, 0, 0, 0};
 #pragma unroll
         for (int e = 0; e < 4; ++e) b[mi][4 * q + e] = v[e];
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) b[mi][4 * q + e] = i + e >= M ? -__builtin_inff() : bias ? bias[i + e] : 0.0f;
+        for (int e = 0; e < 4; ++e) {
+          const float v = bias ? bias[i + e < M ? i + e : M - 1] : 0.0f;
+          b[mi][4 * q + e] = i + e < M ? v : -__builtin_inff();
+        }
       }
     }
 }
@@ -583,29 +627,85 @@ __device__ __forceinline__ void write4(float* p, int64_t left, f32x4 v) {
   }
 }
 
-// A tile of I x J results from its own corner on.
+// A tile of I x J results from its own corner on, in 16 bits.
+template <class T, class Tl>
+__device__ __forceinline__ void write_tile16(typename Tl::Acc& acc, char* lds, T* out, int64_t ldo, int64_t I, int64_t J) {
+  const int lane = threadIdx.x & 63, bi = Tl::base_i(), bj = Tl::base_j();
+  if (Tl::lead()) {
+#pragma unroll
+    for (int nj = 0; nj < Tl::NJ; ++nj)
+#pragma unroll
+      for (int mi = 0; mi < Tl::MI; ++mi)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          stage4<T, Tl>(lds, bi + 32 * mi + entry_row(4 * q, lane), bj + 32 * nj + (lane & 31), acc[mi][nj][4 * q], acc[mi][nj][4 * q + 1],
+                        acc[mi][nj][4 * q + 2], acc[mi][nj][4 * q + 3]);
+  }
+  __syncthreads();
+  write_staged<T, Tl>(lds, out, ldo, I, J);
+}
+
+// The same in 32 bits, through LDS too: in whole lines, and with no sums left
+// in registers around the checks of the matrix's end.  A 256 x 256 tile goes in
+// two halves, columns nj < NJ / 2 of every wavefront's blocks first.  ADD: the
+// results are added to what `sum` [J][lds] holds; T: what is written.
+template <class T, class Tl, bool ADD>
+__device__ __forceinline__ void write_tile32(typename Tl::Acc& acc, char* lds, T* out, int64_t ldo, int64_t I, int64_t J, const float* sum = nullptr,
+                                             int64_t ld_sum = 0) {
+  constexpr int PASSES = Tl::BI * Tl::BJ * 4 > (int)Tl::LDS ? 2 : 1, NP = Tl::NJ / PASSES, ROWS = Tl::BJ / PASSES, C = Tl::BI / 4;
+  static_assert(ROWS * Tl::BI * 4 <= (int)Tl::LDS && NP * PASSES == Tl::NJ, "tile");
+  const int lane = threadIdx.x & 63, bi = Tl::base_i();
+#pragma unroll
+  for (int pass = 0; pass < PASSES; ++pass) {
+    if (pass) __syncthreads();
+    if (Tl::lead()) {
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        const int j = (Tl::wj() * NP + n) * 32 + (lane & 31);   // row of LDS
+#pragma unroll
+        for (int mi = 0; mi < Tl::MI; ++mi)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int c = (bi + 32 * mi + entry_row(4 * q, lane)) >> 2, nj = pass * NP + n;
+            *reinterpret_cast<f32x4*>(lds + (j * C + (c ^ (j & 31))) * 16) =
+                (f32x4){acc[mi][nj][4 * q], acc[mi][nj][4 * q + 1], acc[mi][nj][4 * q + 2], acc[mi][nj][4 * q + 3]};
+          }
+      }
+    }
+    __syncthreads();
+    for (int u = threadIdx.x; u < ROWS * C; u += Tl::NT) {
+      const int row = u / C, c = u % C;
+      const int j = row / (32 * NP) * (32 * Tl::NJ) + pass * (32 * NP) + row % (32 * NP);   // row of the tile
+      const int64_t left = I - c * 4;
+      if (j >= J || left <= 0) continue;
+      f32x4 v = *reinterpret_cast<const f32x4*>(lds + (row * C + (c ^ (row & 31))) * 16);
+      if constexpr (ADD) {
+        const float* p = sum + j * ld_sum + c * 4;
+        if (left >= 4) {
+          v += __builtin_bit_cast(f32x4, load16(p));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (e < left) v[e] += p[e];
+        }
+      }
+      T* to = out + j * ldo + c * 4;
+      if constexpr (sizeof(T) == 4) {
+        write4(to, left, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < left) to[e] = from_float<T>(v[e]);
+      }
+    }
+  }
+}
+
+// as T, whichever that is
 template <class T, class Tl>
 __device__ __forceinline__ void write_tile(typename Tl::Acc& acc, char* lds, T* out, int64_t ldo, int64_t I, int64_t J) {
-  const int lane = threadIdx.x & 63, bi = Tl::base_i(), bj = Tl::base_j();
-#pragma unroll
-  for (int nj = 0; nj < Tl::NJ; ++nj) {
-    const int j = bj + 32 * nj + (lane & 31);
-    if (!Tl::lead()) break;
-#pragma unroll
-    for (int mi = 0; mi < Tl::MI; ++mi)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int i = bi + 32 * mi + entry_row(4 * q, lane);
-        const f32x4 v = {acc[mi][nj][4 * q], acc[mi][nj][4 * q + 1], acc[mi][nj][4 * q + 2], acc[mi][nj][4 * q + 3]};
-        if constexpr (sizeof(T) == 2) stage4<T, Tl>(lds, i, j, v[0], v[1], v[2], v[3]);
-        else if (j < J) write4(out + j * ldo + i, I - i, v);
-        if (sizeof(T) == 4) __builtin_amdgcn_sched_barrier(0);
-      }
-  }
-  if constexpr (sizeof(T) == 2) {
-    __syncthreads();
-    write_staged<T, Tl>(lds, out, ldo, I, J);
-  }
+  if constexpr (sizeof(T) == 2) write_tile16<T, Tl>(acc, lds, out, ldo, I, J);
+  else write_tile32<T, Tl, false>(acc, lds, out, ldo, I, J);
 }
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
