@@ -417,7 +417,8 @@ int maddness_encoder_scatter(const uint8_t* idx, int64_t N, int32_t C,
  *         column 16 mb + i at (mb, kb, i, j); 255: NaN.
  * Rows and columns past the matrix hold code 0 and e = 0.
  * The two functions give the arrays' sizes (-1 for sizes that are not
- * positive).
+ * positive).  Every call on them gives EUNSUPPORTED for D or M above
+ * 2^31 - 129.
  */
 int64_t maddness_w4_code_bytes(int32_t D, int32_t M);
 int64_t maddness_w4_exponent_bytes(int32_t D, int32_t M);

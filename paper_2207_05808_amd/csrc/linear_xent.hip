@@ -471,7 +471,7 @@ hipError_t grad(XArgs a, bool md, void* dA, void* dB, float* dbias, char* ws, hi
     x.first = x.last = 1;
     done = false;
     if constexpr (sizeof(T) == 2) {
-      if (direct(ai, true) && cdiv(a.D, 256) * cdiv(n, 256) >= 192) {
+      if (direct(ai, true) && direct(zi, true) && cdiv(a.D, 256) * cdiv(n, 256) >= 192) {
         done = true;
         e = gemm<T, BigTile<T, kAlongI, kAlongI, false>, false>(x, g.part, s);
       }

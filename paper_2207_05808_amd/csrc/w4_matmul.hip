@@ -731,6 +731,9 @@ hipError_t launch_w4(const WArgs& a, const Many& p, char* ws, hipStream_t stream
 
 using namespace mdn;
 
+// the kernels count rows and columns in 32 bits, whole blocks of them too
+static bool too_large(int32_t D, int32_t M) { return D > INT32_MAX - kWK || M > INT32_MAX - kWK; }
+
 extern "C" {
 
 int64_t maddness_w4_code_bytes(int32_t D, int32_t M) {
@@ -748,6 +751,7 @@ int maddness_quantize_w4(const void* B, int32_t dtype, int32_t D, int32_t M, int
   if (D <= 0 || M <= 0 || stride_d < 0 || stride_m < 0 || !B || !codes_out || !exps_out) return MADDNESS_EINVAL;
   if (dtype < MADDNESS_F32 || dtype > MADDNESS_F16) return MADDNESS_EINVAL;
   if (!aligned(B, dtype == MADDNESS_F32 ? 4 : 2) || !aligned(codes_out, 16) || !aligned(exps_out, 4)) return MADDNESS_EINVAL;
+  if (too_large(D, M)) return MADDNESS_EUNSUPPORTED;
   QArgs a{B, stride_d, stride_m, D, M, (int)(((int64_t)D + kWK - 1) / kWK), (int)(((int64_t)M + kWM - 1) / kWM), codes_out, exps_out};
   hipStream_t s = static_cast<hipStream_t>(stream);
   return status_from(dtype == MADDNESS_F32 ? launch_quantize<float>(a, s) : dtype == MADDNESS_BF16 ? launch_quantize<Bf16>(a, s) : launch_quantize<F16>(a, s));
@@ -758,6 +762,7 @@ int maddness_dequantize_w4(const uint8_t* codes, const uint8_t* exps, int32_t D,
   if (D <= 0 || M <= 0 || !codes || !exps || !B_out) return MADDNESS_EINVAL;
   if (dtype != MADDNESS_F32 && dtype != MADDNESS_BF16) return MADDNESS_EINVAL;
   if (!aligned(B_out, dtype == MADDNESS_F32 ? 4 : 2) || !aligned(codes, 16) || !aligned(exps, 4)) return MADDNESS_EINVAL;
+  if (too_large(D, M)) return MADDNESS_EUNSUPPORTED;
   DArgs a{codes, exps, D, M, (int)(((int64_t)D + kWK - 1) / kWK), (int)(((int64_t)M + kWM - 1) / kWM), B_out};
   const dim3 grid(blocks_for((int64_t)a.nk * ((a.nm + 3) / 4), 1));
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -777,6 +782,7 @@ int maddness_matmul_w4(const void* A, int32_t dtype, int64_t N, int32_t D, int64
   if (N < 0 || D <= 0 || M <= 0 || lda < D || act < 0 || act > 3) return MADDNESS_EINVAL;
   if (dtype < MADDNESS_F32 || dtype > MADDNESS_F16 || (y_dtype != dtype && y_dtype != MADDNESS_F32)) return MADDNESS_EINVAL;
   if (act == MADDNESS_ACT_SOFTMAX && y_dtype != MADDNESS_F32) return MADDNESS_EINVAL;
+  if (too_large(D, M)) return MADDNESS_EUNSUPPORTED;
   if (N == 0) return MADDNESS_OK;
   if (!A || !codes || !exps || !y_out) return MADDNESS_EINVAL;
   if (!aligned(A, dtype == MADDNESS_F32 ? 4 : 2) || !aligned(y_out, y_dtype == MADDNESS_F32 ? 4 : 2) || !aligned(codes, 16) ||

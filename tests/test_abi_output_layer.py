@@ -42,10 +42,10 @@ def test_quantize_rejects(L):
     good = [FAKE, 0, 64, 16, 16, 1, FAKE, FAKE, NULL]
     rejects(L.maddness_quantize_w4, good, [
         (0, NULL, 1), (1, -1, 1), (1, 3, 1), (2, 0, 1), (3, 0, 1), (4, -1, 1), (5, -1, 1), (6, NULL, 1), (7, NULL, 1),
-        (0, at(2), 1), (6, at(8), 1), (7, at(2), 1)])
+        (0, at(2), 1), (6, at(8), 1), (7, at(2), 1), (2, (1 << 31) - 100, 3), (3, (1 << 31) - 100, 3)])
     good = [FAKE, FAKE, 64, 16, FAKE, 1, NULL]
     rejects(L.maddness_dequantize_w4, good, [
-        (0, NULL, 1), (1, NULL, 1), (2, 0, 1), (3, -3, 1), (4, NULL, 1), (5, 2, 1), (5, -1, 1), (0, at(4), 1), (1, at(1), 1), (4, at(1), 1)])
+        (0, NULL, 1), (1, NULL, 1), (2, 0, 1), (3, -3, 1), (4, NULL, 1), (5, 2, 1), (5, -1, 1), (0, at(4), 1), (1, at(1), 1), (4, at(1), 1), (2, (1 << 31) - 1, 3), (3, (1 << 31) - 1, 3)])
 
 
 def test_matmul_rejects(L):
@@ -53,7 +53,7 @@ def test_matmul_rejects(L):
     good = [FAKE, 1, 10, 64, 64, FAKE, FAKE, 16, NULL, 0, FAKE, 1, NULL, 0, NULL]
     rejects(L.maddness_matmul_w4, good, [
         (0, NULL, 1), (1, 3, 1), (1, -1, 1), (2, -1, 1), (3, 0, 1), (4, 63, 1), (5, NULL, 1), (6, NULL, 1), (7, 0, 1), (9, 4, 1), (9, -1, 1),
-        (10, NULL, 1), (11, 2, 1), (0, at(1), 1), (5, at(8), 1), (6, at(2), 1), (8, at(2), 1), (10, at(1), 1)])
+        (10, NULL, 1), (11, 2, 1), (0, at(1), 1), (5, at(8), 1), (6, at(2), 1), (8, at(2), 1), (10, at(1), 1), (7, (1 << 31) - 1, 3)])
     rejects(L.maddness_matmul_w4, good, [(9, 3, 1)])   # a softmax in 16 bits
     assert L.maddness_matmul_w4(NULL, 1, 0, 64, 64, NULL, NULL, 16, NULL, 0, NULL, 1, NULL, 0, NULL) == 0
     size = L.maddness_matmul_w4_workspace_bytes(FAKE, 1, 4000, 64, 64, 512)

@@ -12,6 +12,7 @@ import pytest
 import torch
 
 import paper_2207_05808_amd as mdn
+from paper_2207_05808_amd import _lib
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -154,6 +155,11 @@ def test_many_rows(N, D, M, dtype):
     with pytest.raises(ValueError):
         mdn.matmul_w4(A, w, workspace=ws[:1000])
     z = mdn.matmul_w4(A, w, col_bias=bias, act="relu", out_dtype=torch.float32)
+    none = torch.empty_like(z)
+    st = _lib.lib().maddness_matmul_w4(A.data_ptr(), {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[dtype], N, D, D, w.codes.data_ptr(),
+                                       w.exps.data_ptr(), M, bias.data_ptr(), 2, none.data_ptr(), 0, None, 0, torch.cuda.current_stream().cuda_stream)
+    assert st == 0
+    assert torch.allclose(none, z, rtol=1e-4, atol=1e-4)
     few = torch.cat([mdn.matmul_w4(A[n:n + 64], w, col_bias=bias, act="relu", out_dtype=torch.float32) for n in (0, 64, N - 64)])
     many = torch.cat([z[:128], z[N - 64:]])
     assert torch.allclose(many, few, rtol=1e-4, atol=1e-4)
