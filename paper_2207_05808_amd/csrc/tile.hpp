@@ -340,7 +340,12 @@ struct Tile : Waves<WI_, WJ_, WK, BI_ / WI_ / 32, BJ_ / WJ_ / 32> {
 // quarters that follow.  Reads and transfers are issued between products, a few
 // at a time, since a wavefront waits where the memory pipeline's queue is full.
 // STAGED_X: an operand X whose rows are not whole 16-byte units goes through
-// registers instead.
+// registers instead (15% slower).
+// Measured, 8192 x 4096 x 65536 with the logits reduced in the kernel: 1.36
+// PFLOP/s, where the library's product alone reaches 1.51; two 64-k buffers
+// filled in one burst 1.08, four buffers of 32 k (half lines of rows along k)
+// 1.20.  The matrix cores are busy 70% of the time at 1.8 to 1.9 GHz, the clock
+// that the card holds under them; waits at the barrier take 20%.
 template <class T, Order OX, Order OY, bool STAGED_X>
 struct BigTile : Waves<2, 2, 1, 4, 4> {
   static constexpr int BI = 256, BJ = 256, BK = 64, WI = 2, WJ = 2, MI = 4, NJ = 4, NT = 256;
