@@ -38,8 +38,9 @@ struct Operand {
 // first of them writes).
 template <int WI, int WJ, int WK, int MI, int NJ>
 struct Waves {
-  static __device__ __forceinline__ int wave() { return (threadIdx.x >> 6) % (WI * WJ); }
-  static __device__ __forceinline__ int wk() { return WK == 1 ? 0 : (threadIdx.x >> 6) / (WI * WJ); }
+  // (read as scalars, so that the compiler knows them the same in every lane)
+  static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % (WI * WJ); }
+  static __device__ __forceinline__ int wk() { return WK == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / (WI * WJ); }
   static __device__ __forceinline__ bool lead() { return WK == 1 || wk() == 0; }
   static __device__ __forceinline__ int wi() { return wave() / WJ; }
   static __device__ __forceinline__ int wj() { return wave() % WJ; }

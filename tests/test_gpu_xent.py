@@ -131,7 +131,8 @@ def test_forward_and_gradient(N, D, M, dtype, md):
                                             (5000, 48, 9000, torch.bfloat16, False), (4200, 40, 9001, torch.float32, True),
                                             (40, 96, 70001, torch.bfloat16, False), (9000, 264, 4100, torch.bfloat16, True),
                                             (600, 600, 25001, torch.bfloat16, False), (600, 601, 25001, torch.bfloat16, True),
-                                            (600, 616, 25000, torch.bfloat16, True), (520, 600, 30011, torch.bfloat16, True),
+                                            (600, 616, 25000, torch.bfloat16, True), (520, 600, 30011, torch.bfloat16, True), (600, 601, 25001, torch.bfloat16, False),
+                                            (700, 75, 9001, torch.float32, False), (700, 75, 9001, torch.float32, True),
                                             (9000, 1032, 30001, torch.bfloat16, False), (9001, 1000, 30000, torch.bfloat16, True)])
 def test_larger(N, D, M, dtype, md):
     """More tiles than the card has compute units, whole 16-byte rows and odd
