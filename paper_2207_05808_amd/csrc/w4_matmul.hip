@@ -657,7 +657,7 @@ constexpr int64_t many_rows(int32_t dtype) { return dtype == MADDNESS_BF16 ? 153
 // The plan for many rows; bytes: workspace, 0 where the rows kernel takes the call.
 struct Many {
   int parts; bool direct;   // 16-bit parts of A; A's rows go to LDS as they are
-  int64_t per, piece, off_shift, off_w, bytes;
+  int64_t per, rows, piece, off_shift, off_w, bytes;
 };
 Many plan_many(const void* A, int32_t dtype, int64_t N, int32_t D, int64_t lda, int32_t M) {
   Many p{};
@@ -665,11 +665,15 @@ Many plan_many(const void* A, int32_t dtype, int64_t N, int32_t D, int64_t lda, 
   p.parts = dtype == MADDNESS_F32 ? 3 : 1;
   p.direct = dtype != MADDNESS_F32 && D % 64 == 0 && direct(Operand{A, lda, N, N, 0}, false);
   p.per = ((int64_t)D + kWK - 1) / kWK * kWK;
+  // rows at a time whose parts are made: 256 MiB of them, at least 4096
+  p.rows = (128ll << 20) / (p.parts * p.per) / 256 * 256;
+  if (p.rows < 4096) p.rows = 4096;
+  if (p.direct || p.rows > N) p.rows = N;
   // outputs at a time: their 16-bit weights within 256 MiB, at least 256 outputs
   p.piece = (128ll << 20) / p.per / 256 * 256;
   if (p.piece < 256) p.piece = 256;
   if (p.piece > up(M, 16)) p.piece = up(M, 16);
-  int64_t off = p.direct ? 0 : up(N * p.parts * p.per * 2, 256);
+  int64_t off = p.direct ? 0 : up(p.rows * p.parts * p.per * 2, 256);
   p.off_shift = off;
   off += dtype == MADDNESS_F16 ? up(p.piece * 4, 256) : 0;
   p.off_w = off;
@@ -688,36 +692,36 @@ hipError_t launch_tile(WTArgs& a, hipStream_t s) {
 template <class A, class T, class Y>
 hipError_t launch_many(const WArgs& a, const Many& p, char* ws, hipStream_t s) {
   WTArgs t{};
-  t.A = Operand{a.A, a.lda, a.N, a.N, 0};
-  t.K = a.D;
-  if (!p.direct) {
-    PArgs q{a.A, a.N, a.lda, a.D, ws, p.parts * p.per, (int)p.per};
-    hipLaunchKernelGGL((w4_parts_kernel<A>), dim3(blocks_for(a.N * (p.per / 8), 256)), dim3(256), 0, s, q);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    t.A = Operand{ws, p.parts * p.per, a.N, a.N, 0};
-    t.K = p.parts * p.per;
-  }
-  t.N = a.N; t.act = a.act; t.ldy = a.M;
+  t.act = a.act; t.ldy = a.M;
   t.shift = reinterpret_cast<int32_t*>(ws + p.off_shift);
-  for (int64_t m0 = 0; m0 < a.M; m0 += p.piece) {
-    const int64_t n = a.M - m0 < p.piece ? a.M - m0 : p.piece, at = m0 / kWM * a.nk;
-    EArgs e{a.codes + at * 1024, a.exps + at * 64, a.nk, n, ws + p.off_w, p.per, reinterpret_cast<int32_t*>(ws + p.off_shift)};
-    hipLaunchKernelGGL((w4_unpack_kernel<T>), dim3((unsigned)cdiv(n, kWM)), dim3(256), 0, s, e);
-    hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
-    t.W = Operand{ws + p.off_w, p.per, n, n, p.per};
-    t.M = n;
-    t.bias = a.bias ? a.bias + m0 : nullptr;
-    t.y = static_cast<Y*>(a.y) + m0;
-    // 256 x 256 tiles where they leave work for most compute units
-    if (p.direct || p.parts * p.per <= (1 << 22)) {
-      if (a.N >= 192 && cdiv(a.N, 256) * cdiv(n, 256) >= 192) err = launch_tile<T, Y, BigTile<T, kAlongK, kAlongK, false>>(t, s);
-      else err = launch_tile<T, Y, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>>(t, s);
-    } else {
-      err = launch_tile<T, Y, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>>(t, s);
+  const bool wide = p.direct || p.parts * p.per <= (1 << 22);   // offsets of a 256 x 256 tile fit in 32 bits
+  for (int64_t n0 = 0; n0 < a.N; n0 += p.rows) {
+    t.N = a.N - n0 < p.rows ? a.N - n0 : p.rows;
+    t.A = Operand{a.A, a.lda, t.N, t.N, 0};
+    t.K = a.D;
+    if (!p.direct) {
+      PArgs q{static_cast<const A*>(a.A) + n0 * a.lda, t.N, a.lda, a.D, ws, p.parts * p.per, (int)p.per};
+      hipLaunchKernelGGL((w4_parts_kernel<A>), dim3(blocks_for(t.N * (p.per / 8), 256)), dim3(256), 0, s, q);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      t.A = Operand{ws, p.parts * p.per, t.N, t.N, 0};
+      t.K = p.parts * p.per;
     }
-    if (err != hipSuccess) return err;
+    for (int64_t m0 = 0; m0 < a.M; m0 += p.piece) {
+      const int64_t n = a.M - m0 < p.piece ? a.M - m0 : p.piece, at = m0 / kWM * a.nk;
+      EArgs e{a.codes + at * 1024, a.exps + at * 64, a.nk, n, ws + p.off_w, p.per, reinterpret_cast<int32_t*>(ws + p.off_shift)};
+      hipLaunchKernelGGL((w4_unpack_kernel<T>), dim3((unsigned)cdiv(n, kWM)), dim3(256), 0, s, e);
+      hipError_t err = hipGetLastError();
+      if (err != hipSuccess) return err;
+      t.W = Operand{ws + p.off_w, p.per, n, n, p.per};
+      t.M = n;
+      t.bias = a.bias ? a.bias + m0 : nullptr;
+      t.y = static_cast<Y*>(a.y) + n0 * a.M + m0;
+      // 256 x 256 tiles where they leave work for most compute units
+      if (wide && t.N >= 192 && cdiv(t.N, 256) * cdiv(n, 256) >= 192) err = launch_tile<T, Y, BigTile<T, kAlongK, kAlongK, false>>(t, s);
+      else err = launch_tile<T, Y, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>>(t, s);
+      if (err != hipSuccess) return err;
+    }
   }
   return hipSuccess;
 }

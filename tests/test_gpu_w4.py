@@ -142,11 +142,12 @@ def test_matmul(N, D, M, dtype):
     check(rand((N, D), 4, dtype), w, None, "none")
 
 
-@pytest.mark.parametrize("N,D,M", [(2500, 128, 5000), (3000, 321, 4099), (1600, 64, 30003)])
+@pytest.mark.parametrize("N,D,M", [(2500, 128, 5000), (3000, 321, 4099), (1600, 64, 30003), (12000, 4000, 40)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
 def test_many_rows(N, D, M, dtype):
-    """More tiles than compute units; with the caller's workspace (dirty) and
-    with none at all, which takes the kernel of few rows."""
+    """More tiles than compute units, and fp32 rows whose parts are made in two
+    turns; with the caller's workspace (dirty) and with none at all, which takes
+    the kernel of few rows."""
     w = mdn.quantize_w4(rand((D, M), 3) * D ** -0.5)
     A, bias = rand((N, D), 4, dtype), rand((M,), 5)
     y = check(A, w, bias, "relu")
