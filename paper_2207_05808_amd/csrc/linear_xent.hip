@@ -37,7 +37,7 @@ struct XArgs {
   float2* part;             // [N][tiles]: a tile's maximum and sum
   float* zt;                // [N]: the target's logit
   float* loss; float* lse_out;   // [N] (forward)
-  int64_t m0, m1;           // outputs of this piece (gradient)
+  int64_t m0;               // first output of this piece (gradient)
   const float* lse; const float* gloss;
   void* dz; int64_t ldz;    // [N][ldz]: the piece's G
   float* cpart;             // [row tiles][ldz]: sums of G over a tile's rows
@@ -363,7 +363,8 @@ hipError_t logits(XArgs& a, int64_t outputs, int rows, bool md, hipStream_t s) {
                              : launch_logits<T, GRAD, Tile<T, kAlongI, kAlongK, 128, 128, 2, 2>>(a, outputs, s);
   // Where every workgroup has a compute unit to itself: twice the wavefronts,
   // each for half of the k of a step twice as long, since one wavefront to a SIMD
-  // waits for the stages of a step in turn.
+  // waits for the stages of a step in turn (fp32 10000 x 512 -> 100, 157 workgroups:
+  // 20.8 against 24.2 us; 20000 rows, 313 of them: 41 against 32 without).
   const bool alone = cdiv(a.N, rows) * cdiv(outputs, 128) <= 256;
   constexpr int BK = sizeof(T) == 2 ? 64 : 32;
   if (rows == 64) {
@@ -427,8 +428,10 @@ GradPlan grad_plan(int64_t N, int64_t D, int64_t M, int64_t elem) {
   g.off_dz = take(N * g.p * elem);
   g.off_c = take(cdiv(N, 32) * g.p * 4);
   g.off_sum = take(g.p < M ? N * D * 4 : 0);
-  // shares of a product: a tile of 256 x 256 for each compute unit
-  g.part = 256ll * 256 * 256 * 4;
+  // shares of a product: at most 64 of its results, or a tile of 256 x 256 for
+  // each compute unit
+  const int64_t results = (N > g.p ? N : g.p) * D;
+  g.part = results < 256 * 1024 ? results * 64 * 4 : 256ll * 256 * 256 * 4;
   g.off_part = take(g.part);
   g.total = off;
   return g;
@@ -469,9 +472,12 @@ hipError_t grad(XArgs a, bool md, void* dA, void* dB, float* dbias, char* ws, hi
         else e = md ? gemm<T, BigTile<T, kAlongI, kAlongK, true>, true>(x, g.part, s) : gemm<T, BigTile<T, kAlongK, kAlongK, true>, true>(x, g.part, s);
       }
     }
+    // 64 rows where 128 give less than two rounds of workgroups (fp32, 316 tiles of
+    // 10000 x 512 -> 100: the gradients 71 against 76 us; 512 tiles of 8192 x 1024
+    // -> 1000: 371 with 128 against 380; only short products, 20000 x 512 -> 100,
+    // would gain past that: 103 against 96)
     if (done) {}
     else if (cdiv(a.N, 128) * cdiv(a.D, 128) < 512) e = md ? gemm<T, Tile<T, kAlongI, kAlongK, 128, 64, 2, 2>, true>(x, g.part, s) : gemm<T, Tile<T, kAlongK, kAlongK, 128, 64, 2, 2>, true>(x, g.part, s);
-    else if (a.N <= 32) e = md ? gemm<T, Tile<T, kAlongI, kAlongK, 128, 32, 4, 1>, true>(x, g.part, s) : gemm<T, Tile<T, kAlongK, kAlongK, 128, 32, 4, 1>, true>(x, g.part, s);
     else e = md ? gemm<T, Tile<T, kAlongI, kAlongK, 128, 128, 2, 2>, true>(x, g.part, s) : gemm<T, Tile<T, kAlongK, kAlongK, 128, 128, 2, 2>, true>(x, g.part, s);
     if (e != hipSuccess) return e;
     // dB = A^T G: [D][M] columns m0.., or [M][D] rows m0..
